@@ -67,7 +67,7 @@ typedef enum {
     SPEC_EHIP = -4          /* a HIP call failed */
 } spec_status;
 
-typedef enum { SPEC_F32 = 0, SPEC_BF16 = 1 } spec_dtype;
+typedef enum { SPEC_F32 = 0, SPEC_BF16 = 1, SPEC_E4M3 = 2, SPEC_INT8 = 3 } spec_dtype; /* 2 and 3: 8-bit caches only */
 
 /*
  * Page layouts of the KV cache (the paper leaves the layout to the serving
@@ -320,6 +320,137 @@ spec_status spec_kv_append(const spec_kv_append_args *args, void *hip_stream);
  * SPEC_KV_MFMA layout (dst_k, dst_v; same byte sizes; must not alias the sources). */
 spec_status spec_kv_repack_mfma(const void *src_k, const void *src_v, void *dst_k, void *dst_v,
                                 int32_t num_blocks, int32_t Hkv, int32_t d, void *hip_stream);
+
+/*
+ * The 8-bit cache.  A decode step is bound by the bytes of the cache (Eq. 3's context term); pages of 8-bit codes
+ * with one fp32 scale per (token, KV head) halve them.
+ *
+ *   code = round(x * (M / a)),  scale = a / M,  a = max(largest |x| of the row's d elements, 2^-60)
+ *
+ * with M = 448 for SPEC_E4M3 (8-bit floating point, 4 exponent and 3 mantissa bits, no infinities) and 127 for
+ * SPEC_INT8, rounded to nearest, ties to even; the value of a code is code * scale.  A row that holds a NaN or an infinity
+ * has no scale: its scale is NaN and its codes are 0, so it reads back as NaN and so does every attention row
+ * that sees it (rows that do not see it are not touched).
+ *
+ * Pages hold SPEC_BLOCK_SIZE tokens, in the operand order of the matrix instructions (one byte per element):
+ *   K is [num_blocks][Hkv][d/16][16 tokens][16 dims]: element (token s, dim c) is at (c/16)*256 + s*16 + c%16.
+ *   V is [num_blocks][Hkv][d/64][4 token groups][16 dims][4 dim quarters][4 tokens]: element (s, c) is at
+ *     (((c/64)*4 + s/4)*16 + c%16)*16 + ((c%64)/16)*4 + s%4.
+ *   kv_scale is [num_blocks][Hkv][2][16] fp32: K's scales, then V's.
+ * Slots that hold no visible token may hold anything; a visible token's codes are what spec_kv8_append writes
+ * (the SPEC_E4M3 codes for NaN, 0x7F and 0xFF, are never among them).
+ *
+ * Limits of the four calls below: d in {64, 128}; pools, scales and outputs 32-byte aligned, other rows 16-byte
+ * aligned.  Request slots with no rows (q_len[b] == 0, a padded batch) are allowed everywhere.
+ */
+
+/*
+ * Quantises K and V rows as they enter the cache: row cu_q_len[b] + j goes to token position
+ * kv_len[b] - q_len[b] + j of request b, as in spec_kv_append, for any number of rows per request (a step's k_b + 1,
+ * a prompt).  Everything else in the pools is left as it is.
+ */
+typedef struct {
+    int32_t B, Hkv, d, num_blocks, max_blocks_per_req, T;
+    int32_t src_dtype;            /* SPEC_F32 or SPEC_BF16 */
+    int32_t kv_dtype;             /* SPEC_E4M3 or SPEC_INT8 */
+    int64_t token_stride;         /* elements from one token's rows to the next one's in new_k and new_v (slices of a fused
+                                     projection's output); 0: Hkv * d.  The heads of a token are contiguous. */
+    const void *new_k, *new_v;    /* T tokens of [Hkv][d] */
+    void *k_cache, *v_cache;      /* the pools, written in place */
+    float *kv_scale;
+    const int32_t *block_table;   /* [B][max_blocks_per_req] */
+    const int32_t *kv_len;        /* [B], INCLUDING the rows being appended */
+    const int32_t *cu_q_len;      /* [B+1] */
+    const int32_t *host_kv_len;   /* HOST copy, used for validation only (may be NULL) */
+    const int32_t *host_cu_q_len; /* HOST copy */
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: rows not written because their position fell
+                                     outside the block-table row or their page outside [0, num_blocks) */
+} spec_kv8_append_args;
+spec_status spec_kv8_append(const spec_kv8_append_args *args, void *hip_stream);
+
+/*
+ * Reads tokens of an 8-bit cache back as rows: row cu_len[b] + j of out_k / out_v is token start[b] + j of request b
+ * (a cache that moves to another worker, or into a bf16 pool through spec_kv_append).  The product code * scale is rounded once.
+ */
+typedef struct {
+    int32_t B, Hkv, d, num_blocks, max_blocks_per_req, T;   /* T = cu_len[B] */
+    int32_t kv_dtype;             /* SPEC_E4M3 or SPEC_INT8 */
+    int32_t out_dtype;            /* SPEC_F32 or SPEC_BF16 */
+    const void *k_cache, *v_cache;
+    const float *kv_scale;
+    const int32_t *block_table;   /* [B][max_blocks_per_req] */
+    const int32_t *start;         /* [B] first token read; NULL: 0 */
+    const int32_t *cu_len;        /* [B+1] exclusive prefix sum of the token counts (>= 0) */
+    const int32_t *host_cu_len;   /* HOST copy */
+    void *out_k, *out_v;          /* [T][Hkv][d] */
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: tokens whose position lies outside the
+                                     block-table row or whose page lies outside [0, num_blocks); their rows are zeros */
+} spec_kv8_read_args;
+spec_status spec_kv8_read(const spec_kv8_read_args *args, void *hip_stream);
+
+/*
+ * Lookahead attention over an 8-bit cache: spec_verify_attn's result for the values that the codes stand for.
+ * Scores and output are products of the codes (exact in the matrix instructions' operands) with the scales applied in
+ * fp32.  q is bf16; out is fp32 or bf16.  kv_len[b] may be less than q_len[b] (down to 0): a query row whose position
+ * kv_len[b] - q_len[b] + j is negative sees no key, and its output row is zero.  q_len[b] <= SPEC_K_MAX + 1,
+ * Hq / Hkv <= 16.
+ */
+typedef struct {
+    int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;
+    int32_t kv_dtype;             /* SPEC_E4M3 or SPEC_INT8 */
+    int32_t out_dtype;            /* SPEC_F32: softmax weights as two 16-bit terms; SPEC_BF16: as one */
+    int32_t max_kv_len;           /* length bucket, as in spec_attn_args */
+    int64_t q_token_stride;       /* elements from one token's query rows to the next one's; 0: Hq * d */
+    const void *q;                /* T tokens of [Hq][d] bf16 */
+    const void *k_cache, *v_cache;
+    const float *kv_scale;
+    const int32_t *block_table;   /* [B][max_blocks_per_req] */
+    const int32_t *kv_len;        /* [B], INCLUDING this step's tokens */
+    const int32_t *cu_q_len;      /* [B+1] */
+    void *out;                    /* [T][Hq][d] */
+    const int32_t *host_kv_len;   /* HOST copies (host_kv_len may be NULL if max_kv_len > 0) */
+    const int32_t *host_cu_q_len;
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths do not
+                                     fit the launch (their rows are not written), and block-table entries outside
+                                     [0, num_blocks) (such a page reads as zeros) */
+    float softmax_scale;          /* 0 means 1/sqrt(d) */
+} spec_kv8_attn_args;
+size_t spec_kv8_attn_workspace_bytes(const spec_kv8_attn_args *args);   /* 0 if the arguments are malformed */
+spec_status spec_kv8_attn(const spec_kv8_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Lookahead attention of a batch that comes in groups: the requests cu_group[g] .. cu_group[g+1]-1 have their first
+ * prefix_len[g] tokens (whole pages) in common, and the block-table row of the group's first request says where they
+ * are.  Those tokens are read and multiplied once for all query rows of the group; the tokens after them are each request's own.
+ * The result is spec_verify_attn's (bf16 pools) or spec_kv8_attn's (8-bit pools).  A group of one request or a
+ * prefix of 0 tokens is an ordinary request.  Every query row sees its group's whole prefix: requests with rows have
+ * kv_len[b] - q_len[b] >= prefix_len[g].
+ */
+typedef struct {
+    int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;
+    int32_t G;                    /* groups, G >= 1 */
+    int32_t kv_dtype;             /* SPEC_BF16, SPEC_E4M3 or SPEC_INT8 */
+    int32_t kv_layout;            /* SPEC_BF16: spec_kv_layout; 8-bit pools: SPEC_KV_MFMA */
+    int32_t out_dtype;            /* SPEC_F32: softmax weights as two (bf16 pools: three) 16-bit terms; SPEC_BF16: as one */
+    int32_t max_kv_len;           /* length bucket, as in spec_attn_args: the lengths in kv_len may change under a captured
+                                     launch; the groups and their prefixes are part of the plan */
+    int64_t q_token_stride;       /* as in spec_kv8_attn_args */
+    const void *q;                /* T tokens of [Hq][d] bf16 */
+    const void *k_cache, *v_cache;
+    const float *kv_scale;        /* 8-bit pools; NULL otherwise */
+    const int32_t *block_table;   /* [B][max_blocks_per_req]; the entries of a request's prefix are read from its group's first request only */
+    const int32_t *kv_len;        /* [B], INCLUDING the prefix and this step's tokens */
+    const int32_t *cu_q_len;      /* [B+1] */
+    const int32_t *cu_group;      /* [G+1] exclusive prefix sum of the group sizes (>= 1), cu_group[G] == B */
+    const int32_t *prefix_len;    /* [G] multiples of SPEC_BLOCK_SIZE */
+    void *out;                    /* [T][Hq][d] */
+    const int32_t *host_kv_len;   /* HOST copies (host_kv_len may be NULL if max_kv_len > 0) */
+    const int32_t *host_cu_q_len, *host_cu_group, *host_prefix_len;
+    int64_t *error_count;         /* as in spec_kv8_attn_args; a group whose prefix does not fit the launch is left out whole */
+    float softmax_scale;          /* 0 means 1/sqrt(d) */
+} spec_prefix_attn_args;
+size_t spec_prefix_attn_workspace_bytes(const spec_prefix_attn_args *args);   /* 0 if the arguments are malformed */
+spec_status spec_prefix_attn(const spec_prefix_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Host-side speculation control (Section 4.1, "Using Goodput for Speculation"; no GPU

@@ -27,6 +27,9 @@ def sources():
 # in that file), in parallel with the other sources, and the objects are linked.
 STEP_KERNEL = "step_kernel.hip"
 STEP_PARTS = 5
+# cache_attn.hip: once per kind of cache, and its launch functions (SPEC_CACHE_PART)
+CACHE_KERNEL = "cache_attn.hip"
+CACHE_PARTS = 5
 
 
 def compile_jobs(objdir: str):
@@ -37,10 +40,12 @@ def compile_jobs(objdir: str):
     jobs = []
     for src in sources():
         stem = os.path.splitext(os.path.basename(src))[0]
-        if os.path.basename(src) == STEP_KERNEL:
-            for part in range(STEP_PARTS):
+        name, parts = {STEP_KERNEL: ("SPEC_STEP_PART", STEP_PARTS),
+                       CACHE_KERNEL: ("SPEC_CACHE_PART", CACHE_PARTS)}.get(os.path.basename(src), (None, 0))
+        if parts:
+            for part in range(parts):
                 obj = os.path.join(objdir, "%s_part%d.o" % (stem, part))
-                jobs.append((base + ["-DSPEC_STEP_PART=%d" % part, "-o", obj, src], obj))
+                jobs.append((base + ["-D%s=%d" % (name, part), "-o", obj, src], obj))
         else:
             obj = os.path.join(objdir, stem + ".o")
             jobs.append((base + ["-o", obj, src], obj))

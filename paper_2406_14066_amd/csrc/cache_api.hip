@@ -1,0 +1,366 @@
+// C entry points of the 8-bit cache and of the attention over shared prefixes: argument checks, launch plans.
+#include "cache_ops.h"
+
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <atomic>
+
+namespace specv {
+
+namespace {
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxPacked = (int64_t)1 << 30;   // packed (token, head) rows and work items are 32-bit in the kernels
+constexpr int kPairTokens = 4 * 2 * SPEC_BLOCK_SIZE;   // tokens that a block's wavefronts take at a time
+
+int compute_units()
+{
+    static int cached = 0;
+    if (cached == 0) {
+        int dev = 0, n = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1)
+            n = 256;   // MI355X
+        cached = n;
+    }
+    return cached;
+}
+
+bool aligned(const void *ptr, uintptr_t to) { return (reinterpret_cast<uintptr_t>(ptr) & (to - 1)) == 0; }
+int pages_of(int64_t tokens) { return (int)((tokens + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE); }
+size_t align_up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
+
+// cu[0] = 0 <= cu[1] <= ... <= cu[n] = total
+bool prefix_sum_ok(const int32_t *cu, int n, int total)
+{
+    if (cu[0] != 0 || cu[n] != total) return false;
+    for (int i = 0; i < n; ++i)
+        if (cu[i + 1] < cu[i]) return false;
+    return true;
+}
+
+// ---------------------------------------------------------------------------
+// Append and read
+// ---------------------------------------------------------------------------
+spec_status check_append(const spec_kv8_append_args *a)
+{
+    if (a == nullptr || a->B < 1 || a->Hkv < 1 || a->T < 0 || a->num_blocks < 1 || a->max_blocks_per_req < 1) return SPEC_EINVAL;
+    if (a->new_k == nullptr || a->new_v == nullptr || a->k_cache == nullptr || a->v_cache == nullptr || a->kv_scale == nullptr ||
+        a->block_table == nullptr || a->kv_len == nullptr || a->cu_q_len == nullptr || a->host_cu_q_len == nullptr)
+        return SPEC_EINVAL;
+    if (a->src_dtype != SPEC_F32 && a->src_dtype != SPEC_BF16) return SPEC_EINVAL;
+    if (a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8) return SPEC_EINVAL;
+    if (!aligned(a->k_cache, 32) || !aligned(a->v_cache, 32) || !aligned(a->kv_scale, 32) || !aligned(a->new_k, 16) || !aligned(a->new_v, 16))
+        return SPEC_EINVAL;
+    const int64_t esz = a->src_dtype == SPEC_F32 ? 4 : 2, row = (int64_t)a->Hkv * a->d;
+    if (a->token_stride != 0 && (a->token_stride < row || a->token_stride * esz % 16 != 0)) return SPEC_EINVAL;
+    if (!prefix_sum_ok(a->host_cu_q_len, a->B, a->T)) return SPEC_EINVAL;
+    if (a->host_kv_len != nullptr)
+        for (int b = 0; b < a->B; ++b) {
+            const int n = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b];
+            if (n > 0 && (a->host_kv_len[b] < n || pages_of(a->host_kv_len[b]) > a->max_blocks_per_req)) return SPEC_EINVAL;
+        }
+    if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
+    if (((int64_t)a->T / SPEC_BLOCK_SIZE + 2 * (int64_t)a->B) * a->Hkv > kMaxPacked) return SPEC_EUNSUPPORTED;
+    return SPEC_OK;
+}
+
+spec_status check_read(const spec_kv8_read_args *a)
+{
+    if (a == nullptr || a->B < 1 || a->Hkv < 1 || a->T < 0 || a->num_blocks < 1 || a->max_blocks_per_req < 1) return SPEC_EINVAL;
+    if (a->k_cache == nullptr || a->v_cache == nullptr || a->kv_scale == nullptr || a->block_table == nullptr || a->cu_len == nullptr ||
+        a->host_cu_len == nullptr || a->out_k == nullptr || a->out_v == nullptr)
+        return SPEC_EINVAL;
+    if (a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8) return SPEC_EINVAL;
+    if (a->out_dtype != SPEC_F32 && a->out_dtype != SPEC_BF16) return SPEC_EINVAL;
+    if (!aligned(a->k_cache, 32) || !aligned(a->v_cache, 32) || !aligned(a->kv_scale, 32) || !aligned(a->out_k, 32) || !aligned(a->out_v, 32))
+        return SPEC_EINVAL;
+    if (!prefix_sum_ok(a->host_cu_len, a->B, a->T)) return SPEC_EINVAL;
+    if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
+    if (((int64_t)a->T / SPEC_BLOCK_SIZE + 2 * (int64_t)a->B) * a->Hkv > kMaxPacked) return SPEC_EUNSUPPORTED;
+    return SPEC_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Attention: one set of checks and one plan for both entry points
+// ---------------------------------------------------------------------------
+spec_prefix_attn_args as_prefix_args(const spec_kv8_attn_args *a)   // no groups: G == 0
+{
+    spec_prefix_attn_args x;
+    memset(&x, 0, sizeof x);
+    x.B = a->B; x.Hq = a->Hq; x.Hkv = a->Hkv; x.d = a->d; x.num_blocks = a->num_blocks; x.max_blocks_per_req = a->max_blocks_per_req; x.T = a->T;
+    x.kv_dtype = a->kv_dtype; x.kv_layout = SPEC_KV_MFMA; x.out_dtype = a->out_dtype; x.max_kv_len = a->max_kv_len;
+    x.q_token_stride = a->q_token_stride;
+    x.q = a->q; x.k_cache = a->k_cache; x.v_cache = a->v_cache; x.kv_scale = a->kv_scale;
+    x.block_table = a->block_table; x.kv_len = a->kv_len; x.cu_q_len = a->cu_q_len; x.out = a->out;
+    x.host_kv_len = a->host_kv_len; x.host_cu_q_len = a->host_cu_q_len;
+    x.error_count = a->error_count; x.softmax_scale = a->softmax_scale;
+    return x;
+}
+
+spec_status check_attn(const spec_prefix_attn_args *a)
+{
+    if (a->B < 1 || a->Hq < 1 || a->Hkv < 1 || a->num_blocks < 1 || a->max_blocks_per_req < 1 || a->T < 1) return SPEC_EINVAL;
+    if (a->q == nullptr || a->k_cache == nullptr || a->v_cache == nullptr || a->block_table == nullptr || a->kv_len == nullptr ||
+        a->cu_q_len == nullptr || a->out == nullptr || a->host_cu_q_len == nullptr)
+        return SPEC_EINVAL;
+    if (a->kv_dtype != SPEC_BF16 && a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8) return SPEC_EINVAL;
+    const bool b8 = a->kv_dtype != SPEC_BF16;
+    if ((a->kv_scale != nullptr) != b8) return SPEC_EINVAL;
+    if (a->kv_layout != SPEC_KV_MFMA && (b8 || a->kv_layout != SPEC_KV_TOKEN_MAJOR)) return SPEC_EINVAL;
+    if (a->out_dtype != SPEC_F32 && a->out_dtype != SPEC_BF16) return SPEC_EINVAL;
+    if (!aligned(a->k_cache, 32) || !aligned(a->v_cache, 32) || !aligned(a->kv_scale, 32) || !aligned(a->out, 32) || !aligned(a->q, 16))
+        return SPEC_EINVAL;
+    if (a->max_kv_len < 0 || (a->max_kv_len == 0 && a->host_kv_len == nullptr)) return SPEC_EINVAL;
+    if (pages_of(a->max_kv_len) > a->max_blocks_per_req) return SPEC_EINVAL;
+    if (a->Hq % a->Hkv != 0) return SPEC_EINVAL;
+    if (!(a->softmax_scale >= 0.0f) || isinf(a->softmax_scale)) return SPEC_EINVAL;
+    if (a->q_token_stride != 0 && (a->q_token_stride < (int64_t)a->Hq * a->d || a->q_token_stride % 8 != 0)) return SPEC_EINVAL;
+    if (!prefix_sum_ok(a->host_cu_q_len, a->B, a->T)) return SPEC_EINVAL;
+    if (a->G > 0) {
+        if (a->G > a->B || a->cu_group == nullptr || a->prefix_len == nullptr || a->host_cu_group == nullptr || a->host_prefix_len == nullptr)
+            return SPEC_EINVAL;
+        if (!prefix_sum_ok(a->host_cu_group, a->G, a->B)) return SPEC_EINVAL;
+    }
+    for (int b = 0, g = 0; b < a->B; ++b) {
+        const int n = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b];
+        if (n > SPEC_K_MAX + 1) return SPEC_EINVAL;
+        int prefix = 0;
+        if (a->G > 0) {
+            while (g + 1 < a->G && a->host_cu_group[g + 1] <= b) ++g;
+            prefix = a->host_prefix_len[g];
+            if (b == a->host_cu_group[g] && (prefix < 0 || prefix % SPEC_BLOCK_SIZE != 0 || prefix / SPEC_BLOCK_SIZE > a->max_blocks_per_req))
+                return SPEC_EINVAL;
+            if (a->max_kv_len > 0 && n > 0 && prefix > 0 && prefix + n > a->max_kv_len) return SPEC_EINVAL;
+        }
+        if (a->host_kv_len == nullptr || n == 0) continue;
+        const int len = a->host_kv_len[b];
+        if (len < 0 || pages_of(len) > a->max_blocks_per_req || (a->max_kv_len > 0 && len > a->max_kv_len)) return SPEC_EINVAL;
+        if (prefix > 0 && len - n < prefix) return SPEC_EINVAL;
+    }
+    for (int g = 0; g < a->G; ++g)
+        if (a->host_cu_group[g + 1] == a->host_cu_group[g]) return SPEC_EINVAL;
+    if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
+    if (a->Hq / a->Hkv > 16) return SPEC_EUNSUPPORTED;
+    if ((int64_t)a->T * a->Hq > kMaxPacked) return SPEC_EUNSUPPORTED;
+    return SPEC_OK;
+}
+
+struct Plan {
+    int row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
+    int prefix_tiles, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
+    size_t acc, ml, tickets, prefix_acc, prefix_ml, total;   // offsets into the workspace
+    int64_t blocks, prefix_blocks;
+};
+
+// The chunk length for jobs of `tokens[i]` tokens with `blocks_each[i]` blocks per chunk: the longest of a few that gives
+// at least `want` blocks.
+template <typename F>
+int chunk_length(int most_tokens, int64_t want, F blocks_of)
+{
+    int len = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
+    while (len > 2 * kPairTokens && blocks_of(len) < want) len = std::max(2 * kPairTokens, len / 2 / kPairTokens * kPairTokens);
+    return len;
+}
+
+Plan make_plan(const spec_prefix_attn_args *a)
+{
+    Plan pl;
+    memset(&pl, 0, sizeof pl);
+    const int group = a->Hq / a->Hkv, most_tiles = a->d == 128 ? 2 : 3;
+    const int64_t want = 2 * (int64_t)compute_units();
+    int max_q = 0, max_own = 0, max_len = 0;
+    auto prefix_of = [&](int &g, int b) {
+        if (a->G == 0) return 0;
+        while (g + 1 < a->G && a->host_cu_group[g + 1] <= b) ++g;
+        return (int)a->host_prefix_len[g];
+    };
+    for (int b = 0, g = 0; b < a->B; ++b) {
+        const int n = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = prefix_of(g, b);
+        if (n == 0) continue;
+        const int len = a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b];
+        max_q = std::max(max_q, n);
+        max_own = std::max(max_own, len - prefix);
+        max_len = std::max(max_len, len);
+    }
+    const int max_rows = std::max(max_q * group, 1);
+    pl.max_q_rows = max_rows;
+    pl.capacity = a->max_kv_len > 0 ? a->max_kv_len : max_len;
+    pl.row_tiles = std::min((max_rows + 15) / 16, most_tiles);
+    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
+    pl.chunk_tokens = chunk_length(max_own, want, [&](int len) {
+        int64_t n = 0;
+        for (int b = 0, g = 0; b < a->B; ++b) {
+            const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = prefix_of(g, b);
+            if (q == 0) continue;
+            const int tokens = (a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix;
+            n += std::max((tokens + len - 1) / len, 1) * (int64_t)((q * group + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles));
+        }
+        return n * a->Hkv;
+    });
+    pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
+    pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
+    int max_prefix = 0;
+    int64_t most_rows = 0;
+    for (int g = 0; g < a->G; ++g) {
+        max_prefix = std::max(max_prefix, a->host_prefix_len[g]);
+        most_rows = std::max<int64_t>(most_rows, (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group);
+    }
+    if (max_prefix > 0 && most_rows > 0) {
+        pl.prefix_capacity = max_prefix;
+        pl.prefix_tiles = (int)std::min<int64_t>((most_rows + 15) / 16, most_tiles);
+        auto row_blocks_of = [&](int g) {
+            const int64_t rows = (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group;
+            return (rows + 16 * pl.prefix_tiles - 1) / (16 * pl.prefix_tiles);
+        };
+        for (int g = 0; g < a->G; ++g) pl.prefix_row_blocks += (int)row_blocks_of(g);
+        pl.prefix_chunk_tokens = chunk_length(max_prefix, want, [&](int len) {
+            int64_t n = 0;
+            for (int g = 0; g < a->G; ++g) n += (int64_t)((a->host_prefix_len[g] + len - 1) / len) * row_blocks_of(g);
+            return n * a->Hkv;
+        });
+        pl.max_prefix_chunks = (max_prefix + pl.prefix_chunk_tokens - 1) / pl.prefix_chunk_tokens;
+        pl.prefix_blocks = (int64_t)pl.prefix_row_blocks * a->Hkv * pl.max_prefix_chunks;
+    }
+    const size_t rows = (size_t)a->T * a->Hq;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes); return here; };
+    if (pl.max_chunks > 1) {
+        pl.acc = take(rows * pl.max_chunks * a->d * 4);
+        pl.ml = take(rows * pl.max_chunks * 8);
+        pl.tickets = take((size_t)a->B * a->Hkv * pl.row_blocks * 8);
+    }
+    if (pl.max_prefix_chunks > 0) {
+        pl.prefix_acc = take(rows * pl.max_prefix_chunks * a->d * 4);
+        pl.prefix_ml = take(rows * pl.max_prefix_chunks * 8);
+    }
+    pl.total = std::max(at, kAlign);
+    return pl;
+}
+
+uint32_t next_generation()
+{
+    static std::atomic<uint32_t> counter{0x40000000u};
+    uint32_t g = ++counter;
+    if (g == 0) g = ++counter;
+    return g;
+}
+
+spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const Plan pl = make_plan(a);
+    if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
+    if (pl.blocks > kMaxPacked || pl.prefix_blocks > kMaxPacked) return SPEC_EUNSUPPORTED;
+    char *ws = static_cast<char *>(workspace);
+    CacheAttnParams p;
+    memset(&p, 0, sizeof p);
+    p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.group = a->Hq / a->Hkv; p.num_blocks = a->num_blocks; p.max_blocks_per_req = a->max_blocks_per_req;
+    p.T = a->T;
+    p.G = pl.max_prefix_chunks > 0 ? a->G : 0;   // (groups without a prefix are single requests)
+    p.kind = a->kv_dtype == SPEC_E4M3 ? kCacheE4M3 : a->kv_dtype == SPEC_INT8 ? kCacheInt8 : a->kv_layout == SPEC_KV_MFMA ? kCacheTiles : kCacheTokens;
+    p.d = a->d;
+    p.out_f32 = a->out_dtype == SPEC_F32;
+    p.row_tiles = pl.row_tiles; p.row_blocks = pl.row_blocks; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks;
+    p.capacity_tokens = pl.capacity; p.max_q_rows = pl.max_q_rows;
+    p.prefix_tiles = pl.prefix_tiles; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
+    p.max_prefix_chunks = pl.max_prefix_chunks; p.prefix_capacity = pl.prefix_capacity;
+    p.generation = next_generation();
+    const double scale = a->softmax_scale > 0.0f ? (double)a->softmax_scale : 1.0 / sqrt((double)a->d);
+    p.scale_log2 = (float)(scale * kLog2eD);
+    p.q_stride = a->q_token_stride != 0 ? a->q_token_stride : (int64_t)a->Hq * a->d;
+    p.q = a->q; p.k_cache = a->k_cache; p.v_cache = a->v_cache; p.kv_scale = a->kv_scale;
+    p.block_table = a->block_table; p.kv_len = a->kv_len; p.cu_q_len = a->cu_q_len; p.cu_group = a->cu_group; p.prefix_len = a->prefix_len;
+    p.out = a->out;
+    p.acc = reinterpret_cast<float *>(ws + pl.acc);
+    p.ml = reinterpret_cast<float *>(ws + pl.ml);
+    p.tickets = reinterpret_cast<unsigned long long *>(ws + pl.tickets);
+    p.prefix_acc = reinterpret_cast<float *>(ws + pl.prefix_acc);
+    p.prefix_ml = reinterpret_cast<float *>(ws + pl.prefix_ml);
+    p.errors = reinterpret_cast<unsigned long long *>(a->error_count);
+    return launch_cache_attn(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPEC_OK : SPEC_EHIP;
+}
+
+spec_status check_kv8_attn(const spec_kv8_attn_args *a)
+{
+    if (a == nullptr || (a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8)) return SPEC_EINVAL;
+    const spec_prefix_attn_args x = as_prefix_args(a);
+    return check_attn(&x);
+}
+
+spec_status check_prefix_attn(const spec_prefix_attn_args *a)
+{
+    if (a == nullptr || a->G < 1) return SPEC_EINVAL;
+    return check_attn(a);
+}
+
+}  // namespace
+
+}  // namespace specv
+
+using namespace specv;
+
+extern "C" {
+
+spec_status spec_kv8_append(const spec_kv8_append_args *a, void *hip_stream)
+{
+    const spec_status st = check_append(a);
+    if (st != SPEC_OK || a->T == 0) return st;
+    Kv8AppendParams p;
+    memset(&p, 0, sizeof p);
+    p.B = a->B; p.Hkv = a->Hkv; p.d = a->d; p.max_blocks_per_req = a->max_blocks_per_req; p.num_blocks = a->num_blocks; p.T = a->T;
+    p.src_f32 = a->src_dtype == SPEC_F32;
+    p.int8 = a->kv_dtype == SPEC_INT8;
+    p.token_stride = a->token_stride != 0 ? a->token_stride : (int64_t)a->Hkv * a->d;
+    p.new_k = a->new_k; p.new_v = a->new_v;
+    p.k_cache = static_cast<unsigned char *>(a->k_cache); p.v_cache = static_cast<unsigned char *>(a->v_cache); p.kv_scale = a->kv_scale;
+    p.block_table = a->block_table; p.kv_len = a->kv_len; p.cu_q_len = a->cu_q_len;
+    p.errors = reinterpret_cast<unsigned long long *>(a->error_count);
+    return launch_kv8_append(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPEC_OK : SPEC_EHIP;
+}
+
+spec_status spec_kv8_read(const spec_kv8_read_args *a, void *hip_stream)
+{
+    const spec_status st = check_read(a);
+    if (st != SPEC_OK || a->T == 0) return st;
+    Kv8ReadParams p;
+    memset(&p, 0, sizeof p);
+    p.B = a->B; p.Hkv = a->Hkv; p.d = a->d; p.max_blocks_per_req = a->max_blocks_per_req; p.num_blocks = a->num_blocks; p.T = a->T;
+    p.out_f32 = a->out_dtype == SPEC_F32;
+    p.int8 = a->kv_dtype == SPEC_INT8;
+    p.k_cache = static_cast<const unsigned char *>(a->k_cache); p.v_cache = static_cast<const unsigned char *>(a->v_cache);
+    p.kv_scale = a->kv_scale;
+    p.block_table = a->block_table; p.start = a->start; p.cu_len = a->cu_len;
+    p.out_k = a->out_k; p.out_v = a->out_v;
+    p.errors = reinterpret_cast<unsigned long long *>(a->error_count);
+    return launch_kv8_read(p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPEC_OK : SPEC_EHIP;
+}
+
+size_t spec_kv8_attn_workspace_bytes(const spec_kv8_attn_args *a)
+{
+    if (check_kv8_attn(a) != SPEC_OK) return 0;
+    const spec_prefix_attn_args x = as_prefix_args(a);
+    return make_plan(&x).total;
+}
+
+spec_status spec_kv8_attn(const spec_kv8_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const spec_status st = check_kv8_attn(a);
+    if (st != SPEC_OK) return st;
+    const spec_prefix_attn_args x = as_prefix_args(a);
+    return run_attn(&x, workspace, workspace_bytes, hip_stream);
+}
+
+size_t spec_prefix_attn_workspace_bytes(const spec_prefix_attn_args *a)
+{
+    return check_prefix_attn(a) == SPEC_OK ? make_plan(a).total : 0;
+}
+
+spec_status spec_prefix_attn(const spec_prefix_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const spec_status st = check_prefix_attn(a);
+    if (st != SPEC_OK) return st;
+    return run_attn(a, workspace, workspace_bytes, hip_stream);
+}
+
+}  // extern "C"

@@ -1228,6 +1228,6 @@ const char *spec_status_string(spec_status status)
     return "unknown status";
 }
 
-int32_t spec_verify_version(void) { return 200; }
+int32_t spec_verify_version(void) { return 300; }
 
 }  // extern "C"

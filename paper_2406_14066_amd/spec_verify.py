@@ -21,7 +21,7 @@ BLOCK_SIZE = 16
 NUM_COUNTERS = 8
 
 SPEC_OK, SPEC_EINVAL, SPEC_EUNSUPPORTED, SPEC_EWORKSPACE, SPEC_EHIP = 0, -1, -2, -3, -4
-SPEC_F32, SPEC_BF16 = 0, 1
+SPEC_F32, SPEC_BF16, SPEC_E4M3, SPEC_INT8 = 0, 1, 2, 3   # spec_dtype (the last two: 8-bit caches only)
 KV_TOKEN_MAJOR, KV_MFMA = 0, 1
 ACCEPT_SAMPLE, ACCEPT_GREEDY, ACCEPT_POINT_DRAFT = 0, 1, 2   # spec_accept_mode
 
@@ -68,6 +68,34 @@ class KvAppendArgs(C.Structure):
     ]
 
 
+class Kv8AppendArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "src_dtype", "kv_dtype")] + [
+        ("token_stride", C.c_int64)] + [(n, C.c_void_p) for n in (
+            "new_k", "new_v", "k_cache", "v_cache", "kv_scale", "block_table", "kv_len", "cu_q_len", "host_kv_len", "host_cu_q_len",
+            "error_count")]
+
+
+class Kv8ReadArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "kv_dtype", "out_dtype")] + [
+        (n, C.c_void_p) for n in ("k_cache", "v_cache", "kv_scale", "block_table", "start", "cu_len", "host_cu_len", "out_k", "out_v",
+                                  "error_count")]
+
+
+class Kv8AttnArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "kv_dtype", "out_dtype",
+                                         "max_kv_len")] + [("q_token_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "k_cache", "v_cache", "kv_scale", "block_table", "kv_len", "cu_q_len", "out", "host_kv_len",
+                                  "host_cu_q_len", "error_count")] + [("softmax_scale", C.c_float)]
+
+
+class PrefixAttnArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "G", "kv_dtype", "kv_layout",
+                                         "out_dtype", "max_kv_len")] + [("q_token_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "k_cache", "v_cache", "kv_scale", "block_table", "kv_len", "cu_q_len", "cu_group", "prefix_len",
+                                  "out", "host_kv_len", "host_cu_q_len", "host_cu_group", "host_prefix_len", "error_count")] + [
+        ("softmax_scale", C.c_float)]
+
+
 class PlanInfo(C.Structure):
     _fields_ = [
         ("attn_path", C.c_int32), ("row_tiles", C.c_int32), ("row_groups", C.c_int32),
@@ -91,6 +119,8 @@ EXPORTS = (
     "spec_verify_version", "spec_profile_begin", "spec_profile_end",
     "spec_expected_generated_len", "spec_predict_latency", "spec_fit_latency",
     "spec_acceptance_update", "spec_acceptance_rate", "spec_argmax_goodput",
+    "spec_kv8_append", "spec_kv8_read", "spec_kv8_attn", "spec_kv8_attn_workspace_bytes",
+    "spec_prefix_attn", "spec_prefix_attn_workspace_bytes",
 )
 NUM_KERNELS = 5
 KERNEL_NAMES = ("step", "attn", "attn_generic", "attn_combine", "reject")
@@ -139,6 +169,14 @@ def lib():
         L.spec_profile_begin.restype = C.c_int
         L.spec_profile_end.argtypes = [C.c_void_p, C.c_void_p]
         L.spec_profile_end.restype = C.c_int
+        for name, args in (("spec_kv8_append", Kv8AppendArgs), ("spec_kv8_read", Kv8ReadArgs)):
+            getattr(L, name).argtypes = [C.POINTER(args), C.c_void_p]
+            getattr(L, name).restype = C.c_int
+        for name, args in (("spec_kv8_attn", Kv8AttnArgs), ("spec_prefix_attn", PrefixAttnArgs)):
+            getattr(L, name).argtypes = [C.POINTER(args), C.c_void_p, C.c_size_t, C.c_void_p]
+            getattr(L, name).restype = C.c_int
+            getattr(L, name + "_workspace_bytes").argtypes = [C.POINTER(args)]
+            getattr(L, name + "_workspace_bytes").restype = C.c_size_t
         L.spec_verify_version.argtypes = []
         L.spec_verify_version.restype = C.c_int32
         _lib = L
@@ -335,6 +373,174 @@ def spec_kv_append(new_k, new_v, k_cache, v_cache, block_table, kv_len, cu_q_len
     a, _keep = make_kv_append_args(new_k, new_v, k_cache, v_cache, block_table, kv_len, cu_q_len, host_kv_len,
                                    host_cu_q_len, kv_layout=kv_layout, error_count=error_count)
     spec_kv_append_args(a, stream)
+
+
+# ---------------------------------------------------------------------------
+# The 8-bit cache, and attention over shared prefixes
+# ---------------------------------------------------------------------------
+def _type_of(t, *allowed) -> int:
+    import torch
+    code = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16, torch.float8_e4m3fn: SPEC_E4M3, torch.int8: SPEC_INT8}.get(t.dtype)
+    if code not in allowed:
+        raise TypeError("unsupported dtype %s" % t.dtype)
+    return code
+
+
+def _check_tokens(t, like=None):
+    """Rows [T, heads, d] whose heads and dims are contiguous; tokens may lie further apart (slices of a fused projection)."""
+    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError("rows must be [T, heads, d] with contiguous heads")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or (t.shape[0] > 1 and t.stride(0) != like.stride(0))):
+        raise ValueError("rows must agree in shape, dtype and token stride")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _check_pools(k_cache, v_cache, kv_scale):
+    import torch
+    nb, Hkv, bs, d = k_cache.shape
+    if bs != BLOCK_SIZE or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("pools must be [num_blocks, Hkv, %d, d]" % BLOCK_SIZE)
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("pools must be contiguous")
+    if kv_scale is not None and (tuple(kv_scale.shape) != (nb, Hkv, 2, bs) or kv_scale.dtype != torch.float32 or not kv_scale.is_contiguous()):
+        raise ValueError("kv_scale must be float32 [num_blocks, Hkv, 2, %d]" % BLOCK_SIZE)
+    return nb, Hkv, d
+
+
+def alloc_kv8_pools(num_blocks: int, Hkv: int, d: int, kv_dtype, device="cuda"):
+    """(k_cache, v_cache, kv_scale) of an 8-bit cache; kv_dtype is torch.float8_e4m3fn or torch.int8."""
+    import torch
+    pools = [torch.zeros((num_blocks, Hkv, BLOCK_SIZE, d), dtype=torch.int8, device=device).view(kv_dtype) for _ in range(2)]
+    return pools[0], pools[1], torch.zeros((num_blocks, Hkv, 2, BLOCK_SIZE), dtype=torch.float32, device=device)
+
+
+def make_kv8_append_args(new_k, new_v, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, host_kv_len, host_cu_q_len, *,
+                         error_count=None):
+    """The argument struct of `spec_kv8_append`: rows [T, Hkv, d] (float32 or bfloat16; tokens may be strided) into 8-bit
+    pools [num_blocks, Hkv, 16, d] (float8_e4m3fn or int8) with their scales.  Returns (args, keepalive)."""
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    hc = _host_i32(host_cu_q_len)
+    a = Kv8AppendArgs()
+    a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, v_cache, kv_scale)
+    if tuple(new_k.shape[1:]) != (a.Hkv, a.d):
+        raise ValueError("rows must be [T, %d, %d]" % (a.Hkv, a.d))
+    _check_tokens(new_v)
+    a.token_stride = _check_tokens(new_k, new_v)
+    a.T, a.B = new_k.shape[0], hc.shape[0] - 1
+    a.max_blocks_per_req = block_table.shape[1]
+    a.src_dtype = _type_of(new_k, SPEC_F32, SPEC_BF16)
+    a.kv_dtype = _type_of(k_cache, SPEC_E4M3, SPEC_INT8)
+    a.new_k, a.new_v = new_k.data_ptr(), new_v.data_ptr()
+    a.k_cache, a.v_cache, a.kv_scale = k_cache.data_ptr(), v_cache.data_ptr(), kv_scale.data_ptr()
+    a.block_table, a.kv_len, a.cu_q_len = block_table.data_ptr(), kv_len.data_ptr(), cu_q_len.data_ptr()
+    a.host_kv_len = hk.ctypes.data if hk is not None else None
+    a.host_cu_q_len = hc.ctypes.data
+    a.error_count = _dev_ptr(error_count)
+    return a, (hk, hc, new_k, new_v, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, error_count)
+
+
+def spec_kv8_append(args: Kv8AppendArgs, stream=None) -> None:
+    _check(lib().spec_kv8_append(C.byref(args), _stream_handle(stream)), "spec_kv8_append")
+
+
+def make_kv8_read_args(out_k, out_v, k_cache, v_cache, kv_scale, block_table, start, cu_len, host_cu_len, *, error_count=None):
+    """The argument struct of `spec_kv8_read`: tokens start[b] .. of every request as rows [T, Hkv, d] of out_k and out_v
+    (float32 or bfloat16); start may be None (0).  Returns (args, keepalive)."""
+    hc = _host_i32(host_cu_len)
+    a = Kv8ReadArgs()
+    a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, v_cache, kv_scale)
+    for out in (out_k, out_v):
+        if tuple(out.shape[1:]) != (a.Hkv, a.d) or not out.is_contiguous() or out.shape != out_k.shape or out.dtype != out_k.dtype:
+            raise ValueError("out_k and out_v must be contiguous [T, %d, %d]" % (a.Hkv, a.d))
+    a.T, a.B = out_k.shape[0], hc.shape[0] - 1
+    a.max_blocks_per_req = block_table.shape[1]
+    a.kv_dtype = _type_of(k_cache, SPEC_E4M3, SPEC_INT8)
+    a.out_dtype = _type_of(out_k, SPEC_F32, SPEC_BF16)
+    a.k_cache, a.v_cache, a.kv_scale = k_cache.data_ptr(), v_cache.data_ptr(), kv_scale.data_ptr()
+    a.block_table, a.start, a.cu_len = block_table.data_ptr(), _dev_ptr(start), cu_len.data_ptr()
+    a.host_cu_len = hc.ctypes.data
+    a.out_k, a.out_v = out_k.data_ptr(), out_v.data_ptr()
+    a.error_count = _dev_ptr(error_count)
+    return a, (hc, out_k, out_v, k_cache, v_cache, kv_scale, block_table, start, cu_len, error_count)
+
+
+def spec_kv8_read(args: Kv8ReadArgs, stream=None) -> None:
+    _check(lib().spec_kv8_read(C.byref(args), _stream_handle(stream)), "spec_kv8_read")
+
+
+def _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count):
+    a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, v_cache, kv_scale)
+    _type_of(q, SPEC_BF16)
+    a.q_token_stride = _check_tokens(q)
+    a.T, a.Hq = q.shape[:2]
+    if q.shape[2] != a.d or out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("q and out must be [T, Hq, %d], out contiguous" % a.d)
+    a.B = hc.shape[0] - 1
+    a.max_blocks_per_req = block_table.shape[1]
+    a.out_dtype = _type_of(out, SPEC_F32, SPEC_BF16)
+    a.max_kv_len = max_kv_len
+    a.q, a.k_cache, a.v_cache, a.kv_scale = q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _dev_ptr(kv_scale)
+    a.block_table, a.kv_len, a.cu_q_len, a.out = block_table.data_ptr(), kv_len.data_ptr(), cu_q_len.data_ptr(), out.data_ptr()
+    a.host_kv_len = hk.ctypes.data if hk is not None else None
+    a.host_cu_q_len = hc.ctypes.data
+    a.error_count = _dev_ptr(error_count)
+    a.softmax_scale = softmax_scale
+
+
+def make_kv8_attn_args(q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, host_kv_len, host_cu_q_len, *,
+                       softmax_scale: float = 0.0, max_kv_len: int = 0, error_count=None):
+    """The argument struct of `spec_kv8_attn`: q [T, Hq, d] bfloat16 (tokens may be strided), 8-bit pools with their
+    scales, out [T, Hq, d] float32 or bfloat16.  Returns (args, keepalive)."""
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    hc = _host_i32(host_cu_q_len)
+    a = Kv8AttnArgs()
+    _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count)
+    a.kv_dtype = _type_of(k_cache, SPEC_E4M3, SPEC_INT8)
+    return a, (hk, hc, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, error_count)
+
+
+def _workspace_bytes(name, args) -> int:
+    n = getattr(lib(), name)(C.byref(args))
+    if n == 0:
+        raise SpecVerifyError(SPEC_EINVAL, name)
+    return int(n)
+
+
+def spec_kv8_attn_workspace_bytes(args: Kv8AttnArgs) -> int:
+    return _workspace_bytes("spec_kv8_attn_workspace_bytes", args)
+
+
+def spec_kv8_attn(args: Kv8AttnArgs, workspace, stream=None) -> None:
+    _check(lib().spec_kv8_attn(C.byref(args), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                               _stream_handle(stream)), "spec_kv8_attn")
+
+
+def make_prefix_attn_args(q, k_cache, v_cache, block_table, kv_len, cu_q_len, cu_group, prefix_len, out, host_kv_len, host_cu_q_len,
+                          host_cu_group, host_prefix_len, *, kv_scale=None, kv_layout: int = KV_MFMA, softmax_scale: float = 0.0,
+                          max_kv_len: int = 0, error_count=None):
+    """The argument struct of `spec_prefix_attn`: groups of requests cu_group[g] .. cu_group[g+1]-1 that share their first
+    prefix_len[g] tokens; bfloat16 pools in either layout, or 8-bit pools with kv_scale.  Returns (args, keepalive)."""
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    hc, hg, hp = _host_i32(host_cu_q_len), _host_i32(host_cu_group), _host_i32(host_prefix_len)
+    if hg.shape[0] != hp.shape[0] + 1:
+        raise ValueError("cu_group must have one entry more than prefix_len")
+    a = PrefixAttnArgs()
+    _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count)
+    a.kv_dtype = _type_of(k_cache, SPEC_BF16, SPEC_E4M3, SPEC_INT8)
+    a.kv_layout = kv_layout
+    a.G = hp.shape[0]
+    a.cu_group, a.prefix_len = cu_group.data_ptr(), prefix_len.data_ptr()
+    a.host_cu_group, a.host_prefix_len = hg.ctypes.data, hp.ctypes.data
+    return a, (hk, hc, hg, hp, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, cu_group, prefix_len, out, error_count)
+
+
+def spec_prefix_attn_workspace_bytes(args: PrefixAttnArgs) -> int:
+    return _workspace_bytes("spec_prefix_attn_workspace_bytes", args)
+
+
+def spec_prefix_attn(args: PrefixAttnArgs, workspace, stream=None) -> None:
+    _check(lib().spec_prefix_attn(C.byref(args), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _stream_handle(stream)), "spec_prefix_attn")
 
 
 def spec_profile_begin(max_launches: int) -> None:
