@@ -149,27 +149,59 @@ spec_status check_attn(const spec_prefix_attn_args *a)
 
 struct Plan {
     int row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
-    int prefix_tiles, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
+    int prefix_tiles, prefix_many_rows, prefix_block_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
     size_t acc, ml, tickets, prefix_acc, prefix_ml, total;   // offsets into the workspace
     int64_t blocks, prefix_blocks;
 };
 
-// The chunk length for jobs of `tokens[i]` tokens with `blocks_each[i]` blocks per chunk: the longest of a few that gives
-// at least `want` blocks.
+// Chunk length of jobs that a block streams through, from a model of the launch.  A block takes kBlockUs besides its tokens,
+// kSplitUs more where its job is split (partial results, a ticket, the merge); a token takes kTokenUs while a compute unit has
+// nothing else to do, and its bytes' share of the memory's rate where all units are busy, two blocks each.  The launch
+// ends with its longest block, or when the blocks have gone through their slots.
+constexpr double kBlockUs = 5.5, kSplitUs = 6.0, kTokenUs = 0.0065, kUnitBytesPerUs = 23000.0;
 template <typename F>
-int chunk_length(int most_tokens, int64_t want, F blocks_of)
+int chunk_length(int most_tokens, double token_bytes, F for_each_job)   // for_each_job(f): f(tokens, blocks per chunk)
 {
-    int len = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
-    while (len > 2 * kPairTokens && blocks_of(len) < want) len = std::max(2 * kPairTokens, len / 2 / kPairTokens * kPairTokens);
-    return len;
+    const int most = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
+    const double slots = 2.0 * compute_units(), token_us = 2.0 * token_bytes / kUnitBytesPerUs;
+    int best = most;
+    double best_us = 1e30;
+    for (int len = most; len >= kPairTokens; len = len * 3 / 4 / kPairTokens * kPairTokens) {
+        double longest = 0.0, sum = 0.0;
+        for_each_job([&](int tokens, int64_t blocks) {
+            const int chunks = std::max((tokens + len - 1) / len, 1), each = (tokens + chunks - 1) / chunks;
+            const double fixed = kBlockUs + (chunks > 1 ? kSplitUs : 0.0);
+            longest = std::max(longest, fixed + each * kTokenUs);
+            sum += (double)blocks * chunks * (fixed + each * token_us);
+        });
+        const double us = std::max(longest, sum / slots);
+        if (us < best_us * 0.97) {   // (shorter chunks only for something)
+            best_us = us;
+            best = len;
+        }
+    }
+    return best;
+}
+
+// Steps of a block of the launch for prefixes with many rows: three blocks on each compute unit, which is what fits, and keeps
+// matrix cores and vector units busy at the same time (64 requests behind 4096 tokens, 64/8 heads, k = 2, bf16: one, two, three
+// blocks 62.7 / 51.5 / 44.6 us), unless that leaves a block fewer than 12 steps: then one on each, since every block
+// leaves partial results to write and to read back (11 steps a unit, d = 64, fp32 output: 21.2 + 17.3 us for this launch and the one
+// after it, 19.2 + 25.0 with three).
+int prefix_block_steps(int64_t steps)
+{
+    const int64_t units = compute_units();
+    const int64_t slots = steps >= 3 * units * 12 ? 3 * units : units;
+    const int64_t rounds = (steps + slots * kMaxPrefixPairs - 1) / (slots * kMaxPrefixPairs);
+    return (int)std::max<int64_t>((steps + slots * rounds - 1) / (slots * rounds), 1);
 }
 
 Plan make_plan(const spec_prefix_attn_args *a)
 {
     Plan pl;
     memset(&pl, 0, sizeof pl);
-    const int group = a->Hq / a->Hkv, most_tiles = a->d == 128 ? 2 : 3;
-    const int64_t want = 2 * (int64_t)compute_units();
+    const int group = a->Hq / a->Hkv, most_tiles = 3;
+    const double token_bytes = a->kv_dtype == SPEC_BF16 ? 4.0 * a->d : 2.0 * a->d + 8.0;   // of a KV head
     int max_q = 0, max_own = 0, max_len = 0;
     auto prefix_of = [&](int &g, int b) {
         if (a->G == 0) return 0;
@@ -189,15 +221,12 @@ Plan make_plan(const spec_prefix_attn_args *a)
     pl.capacity = a->max_kv_len > 0 ? a->max_kv_len : max_len;
     pl.row_tiles = std::min((max_rows + 15) / 16, most_tiles);
     pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
-    pl.chunk_tokens = chunk_length(max_own, want, [&](int len) {
-        int64_t n = 0;
+    pl.chunk_tokens = chunk_length(max_own, token_bytes, [&](auto job) {
         for (int b = 0, g = 0; b < a->B; ++b) {
             const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = prefix_of(g, b);
             if (q == 0) continue;
-            const int tokens = (a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix;
-            n += std::max((tokens + len - 1) / len, 1) * (int64_t)((q * group + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles));
+            job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, (int64_t)((q * group + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles)) * a->Hkv);
         }
-        return n * a->Hkv;
     });
     pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
     pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
@@ -209,19 +238,30 @@ Plan make_plan(const spec_prefix_attn_args *a)
     }
     if (max_prefix > 0 && most_rows > 0) {
         pl.prefix_capacity = max_prefix;
-        pl.prefix_tiles = (int)std::min<int64_t>((most_rows + 15) / 16, most_tiles);
-        auto row_blocks_of = [&](int g) {
-            const int64_t rows = (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group;
-            return (rows + 16 * pl.prefix_tiles - 1) / (16 * pl.prefix_tiles);
-        };
-        for (int g = 0; g < a->G; ++g) pl.prefix_row_blocks += (int)row_blocks_of(g);
-        pl.prefix_chunk_tokens = chunk_length(max_prefix, want, [&](int len) {
-            int64_t n = 0;
-            for (int g = 0; g < a->G; ++g) n += (int64_t)((a->host_prefix_len[g] + len - 1) / len) * row_blocks_of(g);
-            return n * a->Hkv;
-        });
-        pl.max_prefix_chunks = (max_prefix + pl.prefix_chunk_tokens - 1) / pl.prefix_chunk_tokens;
-        pl.prefix_blocks = (int64_t)pl.prefix_row_blocks * a->Hkv * pl.max_prefix_chunks;
+        pl.prefix_many_rows = most_rows > 16 * most_tiles;
+        auto rows_of = [&](int g) { return (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group; };
+        if (pl.prefix_many_rows) {
+            auto pairs_of = [&](int g) { return (a->host_prefix_len[g] + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE); };
+            int64_t steps = 0;
+            for (int g = 0; g < a->G; ++g) steps += (rows_of(g) + kPrefixRows - 1) / kPrefixRows * pairs_of(g);
+            steps *= a->Hkv;
+            pl.prefix_block_steps = prefix_block_steps(steps);
+            pl.prefix_blocks = ((steps + pl.prefix_block_steps - 1) / pl.prefix_block_steps + kXcdCount - 1) / kXcdCount * kXcdCount;
+            pl.prefix_row_blocks = (int)pl.prefix_blocks;
+            // partial results of a row block: one of each block that its steps touch
+            pl.max_prefix_chunks = ((max_prefix + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE) + pl.prefix_block_steps - 2) / pl.prefix_block_steps + 1;
+        } else {
+            pl.prefix_tiles = (int)std::min<int64_t>((most_rows + 15) / 16, most_tiles);
+            auto row_blocks_of = [&](int g) { return (rows_of(g) + 16 * pl.prefix_tiles - 1) / (16 * pl.prefix_tiles); };
+            // (as many as the rows can make however they are spread over the groups)
+            pl.prefix_row_blocks = (int)((int64_t)a->T * group / (16 * pl.prefix_tiles)) + a->G;
+            pl.prefix_chunk_tokens = chunk_length(max_prefix, token_bytes, [&](auto job) {
+                for (int g = 0; g < a->G; ++g)
+                    if (a->host_prefix_len[g] > 0) job(a->host_prefix_len[g], row_blocks_of(g) * a->Hkv);
+            });
+            pl.max_prefix_chunks = (max_prefix + pl.prefix_chunk_tokens - 1) / pl.prefix_chunk_tokens;
+            pl.prefix_blocks = (int64_t)pl.prefix_row_blocks * a->Hkv * pl.max_prefix_chunks;
+        }
     }
     const size_t rows = (size_t)a->T * a->Hq;
     size_t at = 0;
@@ -251,7 +291,8 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
 {
     const Plan pl = make_plan(a);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
-    if (pl.blocks > kMaxPacked || pl.prefix_blocks > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if (a->B > 65535 || pl.prefix_row_blocks > 65535 || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
+    if (pl.blocks > kMaxPacked || pl.prefix_blocks * std::max(pl.prefix_block_steps, 1) > kMaxPacked) return SPEC_EUNSUPPORTED;
     char *ws = static_cast<char *>(workspace);
     CacheAttnParams p;
     memset(&p, 0, sizeof p);
@@ -263,9 +304,10 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     p.out_f32 = a->out_dtype == SPEC_F32;
     p.row_tiles = pl.row_tiles; p.row_blocks = pl.row_blocks; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks;
     p.capacity_tokens = pl.capacity; p.max_q_rows = pl.max_q_rows;
-    p.prefix_tiles = pl.prefix_tiles; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
+    p.prefix_tiles = pl.prefix_tiles; p.prefix_many_rows = pl.prefix_many_rows; p.prefix_block_steps = pl.prefix_block_steps; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
     p.max_prefix_chunks = pl.max_prefix_chunks; p.prefix_capacity = pl.prefix_capacity;
     p.generation = next_generation();
+    p.group_inverse = (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group);   // (unused where the group is 1)
     const double scale = a->softmax_scale > 0.0f ? (double)a->softmax_scale : 1.0 / sqrt((double)a->d);
     p.scale_log2 = (float)(scale * kLog2eD);
     p.q_stride = a->q_token_stride != 0 ? a->q_token_stride : (int64_t)a->Hq * a->d;

@@ -25,8 +25,9 @@ namespace specv {
 
 // Variants are chosen by (row tiles, head dim, weights in more than one term); one set per kind of cache.
 struct CacheLaunch {
-    unsigned blocks;
-    int prefix;   // which of the two launches
+    dim3 blocks;
+    int prefix;      // which of the two launches
+    int many_rows;   // the prefix's blocks take 4 * tiles row tiles each
 };
 template <int KIND>
 hipError_t launch_cache_kind(const CacheAttnParams &p, int tiles, bool full, CacheLaunch at, hipStream_t stream);
@@ -37,27 +38,41 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
+constexpr int kDeviceScope = 16;        // "sc1" bit of a raw buffer access: coherent over the device's caches
 constexpr float kRescaleSlack = 8.0f;   // the running reference follows the maximum when it is this much behind
 
 constexpr int v_row_bytes(int D) { return D * 2 + 16; }   // token rows of V in LDS (token-major pages)
-constexpr int o_row_bytes(int D) { return D * 4 + 16; }   // result rows in LDS
+constexpr int q_row_bytes(int D) { return D * 2 + 16; }   // query rows in LDS
+
+// The IEEE 754-2019 maximum: unlike fmaxf it needs no canonicalising multiplication per operand that a matrix
+// instruction made.  A NaN stays one: the row it belongs to is NaN whatever its reference is.
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 template <int KIND, int D>
 struct Pair {   // two pages
     static constexpr int N = is_8bit(KIND) ? D / 64 : D / 32;   // 1 KB loads of K, of V
     u32x4 k[2][N], v[2][N];
-    f32x4 ks[is_8bit(KIND) ? 2 : 1], vs[is_8bit(KIND) ? 2 : 1];
+    float ks, vs;   // 8-bit: the scales of one token: lane (g, n) has token 4 g + n % 4 of page n / 4 % 2
 };
+
+// Lane N of the 16-lane row, to all lanes of the row.
+template <int N>
+__device__ __forceinline__ float row_broadcast(float x)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), 0x150 + N, 0xF, 0xF, true));
+}
 
 template <int KIND, int NT, int D>
 struct Shared {
+    static constexpr int kSlices = D / 16 / kWaves;          // 16-dim slices that a wavefront merges
     union {
-        unsigned char v[KIND == kCacheTokens ? kWaves : 1][KIND == kCacheTokens ? 2 * SPEC_BLOCK_SIZE * v_row_bytes(D) : 16];
-        f32x4 acc[2][NT][D / 16][kWave];                 // results of the wavefronts being merged
-        unsigned char o[NT * 16 * o_row_bytes(D)];       // the block's result, by rows
+        struct {
+            alignas(16) unsigned char q[NT * 16 * q_row_bytes(D)];   // the block's query rows
+            unsigned char v[KIND == kCacheTokens ? kWaves : 1][KIND == kCacheTokens ? 2 * SPEC_BLOCK_SIZE * v_row_bytes(D) : 16];
+        };
+        f32x4 acc[kWaves][kWaves - 1][NT][kSlices][kWave];   // for each wavefront, the others' results for its slices
     };
-    float m[2][NT][kWave], l[2][NT][kWave];
-    float row_m[NT * 16], row_l[NT * 16];
+    float m[kWaves][NT][16], l[kWaves][NT][16];
     int last;
 };
 
@@ -69,9 +84,29 @@ struct Work {
     int row_lo;        // first of them that is this block's
     int tok0, tok1;    // its tokens
     int hide_from;     // row r of the block's rows sees tokens < hide_from + r / group; all of them: INT_MAX
-    int group_index, prefix_chunks;   // partial results that come in from the prefix launch
+    int prefix;        // tokens of its group's prefix
+    int group_index, first_of_group, end_of_group;    // its group, and (lane-wise, groups 0 .. 63) every group's requests and prefix
+    int prefix_of_group;
+    int prefix_chunks;                // partial results that come in from the prefix launch
+    int prefix_base, prefix_pairs;    // ... with many rows: the group's first step on this KV head, the steps of a row block
+    int prefix_row0;                  // ... and its first packed token row
     int row_block;
 };
+
+// r / group for rows: a product with a rounded-up reciprocal, exact for r < 2^32 / 16.
+__device__ __forceinline__ int by_group(const CacheAttnParams &p, int r) { return p.group == 1 ? r : (int)__umulhi((uint32_t)r, p.group_inverse); }
+
+// Packed (token row, query head) of fused row r of the rows that begin at packed token row row0.
+__device__ __forceinline__ size_t packed_row(const CacheAttnParams &p, int row0, int kvh, int r)
+{
+    const int j = by_group(p, r);
+    return (size_t)(row0 + j) * p.Hq + kvh * p.group + (r - j * p.group);
+}
+__device__ __forceinline__ const __bf16 *query_row(const CacheAttnParams &p, int row0, int kvh, int r)
+{
+    const int j = by_group(p, r);
+    return static_cast<const __bf16 *>(p.q) + (size_t)(row0 + j) * p.q_stride + (size_t)(kvh * p.group + (r - j * p.group)) * (p.d);
+}
 
 __device__ __forceinline__ void count_error(const CacheAttnParams &p, bool first)
 {
@@ -99,16 +134,107 @@ __device__ __forceinline__ bool prefix_ok(const CacheAttnParams &p, int len)
 
 __device__ __forceinline__ int chunk_count(int tokens, int chunk_tokens) { return (tokens + chunk_tokens - 1) / chunk_tokens; }
 
-// One block of the own launch.  Items: chunk-major, then row blocks, requests, KV heads innermost.
-template <int NT>
-__device__ __forceinline__ bool place_own(const CacheAttnParams &p, int item, Work &w)
+// Steps of the launch for prefixes with many query rows (see prefix_rows_kernel): of all groups of a KV head in `total`,
+// of the groups before group `upto` as the result.
+__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int b0, int b1, int P, int &pairs, int &rows, int &row0)
 {
-    w.kvh = item % p.Hkv;
-    item /= p.Hkv;
-    w.b = item % p.B;
-    item /= p.B;
-    w.row_block = item % p.row_blocks;
-    w.chunk = item / p.row_blocks;
+    pairs = rows = row0 = 0;
+    if (b0 < 0 || b0 > b1 || b1 > p.B || !prefix_ok(p, P)) return 0;
+    row0 = p.cu_q_len[b0];
+    const int end = p.cu_q_len[b1];
+    rows = (end - row0) * p.group;
+    if (row0 < 0 || end > p.T || rows <= 0) return 0;
+    pairs = (P + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE);
+    return (rows + kPrefixRows - 1) / kPrefixRows * pairs;
+}
+
+__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int g, int &pairs, int &rows)
+{
+    int row0;
+    return group_steps(p, p.cu_group[g], p.cu_group[g + 1], p.prefix_len[g], pairs, rows, row0);
+}
+
+__device__ __forceinline__ int prefix_steps(const CacheAttnParams &p, int upto, int &total)
+{
+    const int lane = threadIdx.x % kWave;
+    int all = 0, before = 0;
+    for (int base = 0; base < p.G; base += kWave) {
+        int pairs, rows, n = base + lane < p.G ? group_steps(p, base + lane, pairs, rows) : 0;
+        int some = base + lane < upto ? n : 0;
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) {
+            n += __shfl_xor(n, off);
+            some += __shfl_xor(some, off);
+        }
+        all += n;
+        before += some;
+    }
+    total = __builtin_amdgcn_readfirstlane(all);
+    return __builtin_amdgcn_readfirstlane(before);
+}
+
+struct PrefixPlace {
+    int request, row0, rows;    // the group's first request, its first packed token row, its fused query rows
+    int row_block, first;       // row block of the step, and the step's pair of pages
+    int pairs, pages;           // of the prefix
+};
+
+// The groups base .. base + 63, a lane each.
+struct GroupLanes {
+    int b0, pages, row0, rows, pairs;
+    int steps, upto;   // of the group; of it and the lanes before it
+    __device__ __forceinline__ void look(const CacheAttnParams &p, int base)
+    {
+        const int lane = threadIdx.x % kWave, g = base + lane;
+        steps = b0 = pages = row0 = rows = pairs = 0;
+        if (g < p.G) {
+            b0 = p.cu_group[g];
+            const int b1 = p.cu_group[g + 1], P = p.prefix_len[g];
+            steps = group_steps(p, b0, b1, P, pairs, rows, row0);
+            pages = P / SPEC_BLOCK_SIZE;
+        }
+        upto = steps;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const int up = __shfl_up(upto, off);
+            if (lane >= off) upto += up;
+        }
+    }
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, kWave - 1); }
+    // step `step`, counted from these groups' first; false: it lies after them
+    __device__ __forceinline__ bool find(int step, PrefixPlace &at) const
+    {
+        const unsigned long long holds = __builtin_amdgcn_ballot_w64(upto > step);
+        if (holds == 0) return false;
+        const int who = __builtin_ctzll(holds);
+        const int rest = step - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(steps, who));
+        at.pairs = __builtin_amdgcn_readlane(pairs, who);
+        at.rows = __builtin_amdgcn_readlane(rows, who);
+        at.row0 = __builtin_amdgcn_readlane(row0, who);
+        at.request = __builtin_amdgcn_readlane(b0, who);
+        at.pages = __builtin_amdgcn_readlane(pages, who);
+        at.row_block = rest / at.pairs;
+        at.first = rest - at.row_block * at.pairs;
+        return true;
+    }
+};
+
+// One block of the own launch: grid (KV heads, requests, row blocks x chunks).
+template <int NT>
+__device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
+{
+    w.kvh = blockIdx.x;
+    w.b = blockIdx.y;
+    w.chunk = p.row_blocks == 1 ? blockIdx.z : blockIdx.z / p.row_blocks;
+    w.row_block = blockIdx.z - w.chunk * p.row_blocks;
+    // (up to 64 groups, a lane each, are looked up with the loads that the lengths take anyway)
+    const int lane = threadIdx.x % kWave;
+    w.first_of_group = w.end_of_group = w.prefix_of_group = 0;
+    if (p.G <= kWave && lane < p.G) {
+        w.first_of_group = p.cu_group[lane];
+        w.end_of_group = p.cu_group[lane + 1];
+        w.prefix_of_group = p.prefix_len[lane];
+    }
     const int L = uniform_load(p.kv_len, w.b);
     w.row0 = uniform_load(p.cu_q_len, w.b);
     const int q_len = uniform_load(p.cu_q_len, w.b + 1) - w.row0;
@@ -116,10 +242,14 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, int item, Wo
     const bool first = w.chunk == 0 && w.kvh == 0 && w.row_block == 0;
     int P = 0;
     w.group_index = 0;
-    if (p.G > 0) {
+    if (p.G > kWave) {
         w.group_index = group_of(p, w.b);
         P = uniform_load(p.prefix_len, w.group_index);
+    } else if (p.G > 0) {
+        w.group_index = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < p.G && w.end_of_group <= w.b)), p.G - 1);
+        P = __builtin_amdgcn_readlane(w.prefix_of_group, w.group_index);
     }
+    w.prefix = P;
     // The lengths come from device memory and bound every loop and index below: a request whose lengths do not fit
     // the launch is left out and reported.
     if (q_len < 0 || q_len > SPEC_K_MAX + 1 || w.row0 < 0 || w.row0 + q_len > p.T || q_len * p.group > p.max_q_rows || L < 0 ||
@@ -131,12 +261,11 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, int item, Wo
     w.rows = q_len * p.group;
     w.row_lo = w.row_block * (NT * 16);
     if (w.row_lo >= w.rows) return false;
-    w.prefix_chunks = P > 0 ? chunk_count(P, p.prefix_chunk_tokens) : 0;
     // even chunks per request, page aligned; a request without tokens has one that is empty
     const int tokens = L - P;
-    w.nchunks = max(min(chunk_count(tokens, p.chunk_tokens), p.max_chunks), 1);
+    w.nchunks = p.max_chunks == 1 ? 1 : max(min(chunk_count(tokens, p.chunk_tokens), p.max_chunks), 1);
     if (w.chunk >= w.nchunks) return false;
-    const int C = ((tokens + w.nchunks - 1) / w.nchunks + SPEC_BLOCK_SIZE - 1) & ~(SPEC_BLOCK_SIZE - 1);
+    const int C = w.nchunks == 1 ? tokens : ((tokens + w.nchunks - 1) / w.nchunks + SPEC_BLOCK_SIZE - 1) & ~(SPEC_BLOCK_SIZE - 1);
     if (C > kMaxChunkTokens) {   // (a prefix that is shorter on the device than planned for)
         count_error(p, first);
         return false;
@@ -147,14 +276,55 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, int item, Wo
     return true;
 }
 
-// One block of the prefix launch.  Items: chunk-major, then row blocks of all groups, KV heads innermost.
-template <int NT>
-__device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, int item, Work &w)
+// Which partial results of the prefix launch are this block's (not needed before its own rows are done, so it is found out while
+// the first pages are on their way).  False: they are not there; reported.
+__device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w)
 {
-    w.kvh = item % p.Hkv;
-    item /= p.Hkv;
-    const int block = item % p.prefix_row_blocks;
-    w.chunk = item / p.prefix_row_blocks;
+    w.prefix_chunks = 0;
+    w.prefix_pairs = 0;
+    if (w.prefix == 0) return true;
+    if (!p.prefix_many_rows) {
+        w.prefix_chunks = chunk_count(w.prefix, p.prefix_chunk_tokens);
+        return true;
+    }
+    int total, before, rows;
+    if (p.G <= kWave) {
+        const int lane = threadIdx.x % kWave;
+        int pairs = 0, all_rows = 0, row0 = 0;
+        int n = lane < p.G ? group_steps(p, w.first_of_group, w.end_of_group, w.prefix_of_group, pairs, all_rows, row0) : 0;
+        int some = lane < w.group_index ? n : 0;
+        w.prefix_pairs = __builtin_amdgcn_readlane(n, w.group_index) > 0 ? __builtin_amdgcn_readlane(pairs, w.group_index) : 0;
+        rows = __builtin_amdgcn_readlane(all_rows, w.group_index);
+        w.prefix_row0 = __builtin_amdgcn_readlane(row0, w.group_index);
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) {
+            n += __shfl_xor(n, off);
+            some += __shfl_xor(some, off);
+        }
+        total = __builtin_amdgcn_readfirstlane(n);
+        before = __builtin_amdgcn_readfirstlane(some);
+    } else {
+        before = prefix_steps(p, w.group_index, total);
+        if (group_steps(p, w.group_index, w.prefix_pairs, rows) == 0) w.prefix_pairs = 0;
+        w.prefix_row0 = w.prefix_pairs > 0 ? uniform_load(p.cu_q_len, uniform_load(p.cu_group, w.group_index)) : 0;
+    }
+    const int after = (w.row0 - w.prefix_row0) * p.group;   // the request's rows lie in its group's
+    if ((int64_t)total * p.Hkv > (int64_t)p.prefix_row_blocks * p.prefix_block_steps || w.prefix_pairs == 0 || after < 0 ||
+        after + w.rows > rows) {
+        count_error(p, w.chunk == 0 && w.kvh == 0 && w.row_block == 0);
+        return false;
+    }
+    w.prefix_base = w.kvh * total + before;
+    return true;
+}
+
+// One block of the prefix launch: grid (KV heads, row blocks of all groups, chunks).
+template <int ROWS>
+__device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, Work &w)
+{
+    w.kvh = blockIdx.x;
+    const int block = blockIdx.y;
+    w.chunk = blockIdx.z;
     // the group that holds row block `block`: a lane counts the blocks of a group, 64 groups at a time
     const int lane = threadIdx.x % kWave;
     int before = 0, g = -1;
@@ -164,7 +334,7 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, int item,
             const int b0 = p.cu_group[base + lane], b1 = p.cu_group[base + lane + 1];
             if (b0 >= 0 && b0 <= b1 && b1 <= p.B) {
                 const int rows = (p.cu_q_len[b1] - p.cu_q_len[b0]) * p.group;
-                n = rows > 0 ? (rows + NT * 16 - 1) / (NT * 16) : 0;
+                n = rows > 0 ? (rows + ROWS - 1) / ROWS : 0;
             }
         }
         int sum = n;   // inclusive prefix sum over the lanes
@@ -192,7 +362,7 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, int item,
     const int tokens = uniform_load(p.cu_q_len, b1) - w.row0;
     if (!prefix_ok(p, P) || P == 0 || w.row0 < 0 || tokens < 0 || w.row0 + tokens > p.T) return false;   // (counted by the own launch)
     w.rows = tokens * p.group;
-    w.row_lo = w.row_block * (NT * 16);
+    w.row_lo = w.row_block * ROWS;
     if (w.row_lo >= w.rows) return false;
     w.nchunks = chunk_count(P, p.prefix_chunk_tokens);
     if (w.chunk >= w.nchunks) return false;
@@ -200,45 +370,32 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, int item,
     w.tok0 = min(w.chunk * C, P);
     w.tok1 = min(w.tok0 + C, P);
     w.hide_from = 0x7FFFFFFF - SPEC_K_MAX - 1;
-    w.prefix_chunks = 0;
+    w.prefix = 0;
     return true;
 }
 
-// Weighted sum of the partial results of a row, four head dims per thread.
+// Weighted sum of partial results: N times four head dims of a row.
+template <int N>
 struct RowSum {
-    float m = kEmptyMax, l = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    __device__ __forceinline__ void add(float pm, float pl, f32x4 po)
+    float m, l;
+    f32x4 o[N];
+    __device__ __forceinline__ void clear()
+    {
+        m = kEmptyMax;
+        l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __device__ __forceinline__ void add(float pm, float pl, const f32x4 (&po)[N])
     {
         const float mn = fmaxf(m, pm);
         const float keep = fast_exp2(m - mn), take = fast_exp2(pm - mn);
         l = l * keep + pl * take;
-        o = o * keep + po * take;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = o[i] * keep + po[i] * take;
         m = mn;
     }
 };
-
-template <int D>
-__device__ __forceinline__ void add_prefix(const CacheAttnParams &p, RowSum &sum, size_t rh, int chunks, int dim)
-{
-    for (int c = 0; c < chunks; ++c) {
-        const size_t slot = rh * p.max_prefix_chunks + c;
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
-        sum.add(ml.x, ml.y, *reinterpret_cast<const f32x4 *>(p.prefix_acc + slot * D + dim));
-    }
-}
-
-template <int D>
-__device__ __forceinline__ void write_row(const CacheAttnParams &p, size_t rh, int dim, const RowSum &sum)
-{
-    const float inv = sum.l == 0.0f ? 0.0f : 1.0f / sum.l;   // (a row that has seen no key is zero)
-    const f32x4 o = sum.o * inv;
-    if (p.out_f32)
-        __builtin_nontemporal_store(o, reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + rh * D + dim));
-    else
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, __builtin_convertvector(o, bf16x4)),
-                                    reinterpret_cast<u32x2 *>(static_cast<__bf16 *>(p.out) + rh * D + dim));
-}
 
 template <int KIND, int NT, int D, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams p, int prefix)
@@ -252,13 +409,21 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     __shared__ Shared<KIND, NT, D> sh;
 
     Work w;
-    if (!(prefix ? place_prefix<NT>(p, blockIdx.x, w) : place_own<NT>(p, blockIdx.x, w))) return;
+    if (!(prefix ? place_prefix<NT * 16>(p, w) : place_own<NT>(p, w))) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, g = lane >> 4;
     const int rows = min(w.rows - w.row_lo, NT * 16);   // this block's
-    auto out_index = [&](int r) {   // packed (token row, query head) of the block's row r
-        const int rr = w.row_lo + r;
-        return (size_t)(w.row0 + rr / p.group) * p.Hq + w.kvh * p.group + rr % p.group;
-    };
+
+    // Q goes to LDS and comes back as the B operand of S^T = K Q^T when it is needed, which keeps registers for pages on
+    // their way: lane (g, n) takes row n, the 8 dims that the lane's K holds (bf16 pages: 32 kk + 8 g ..; 8-bit pages, 16
+    // bytes of which are two operands: 64 (kk / 2) + 16 g + 8 (kk % 2) ..)
+    constexpr int QP = D / 8, QN = (NT * 16 * QP + kThreads - 1) / kThreads;   // 16-byte pieces of a row, of a thread
+    u32x4 q_piece[QN];
+#pragma unroll
+    for (int k = 0; k < QN; ++k) {
+        const int piece = k * kThreads + tid, r = piece / QP;
+        q_piece[k] = (u32x4){0u, 0u, 0u, 0u};
+        if (r < rows) q_piece[k] = *reinterpret_cast<const u32x4 *>(query_row(p, w.row0, w.kvh, w.row_lo + r) + piece % QP * 8);
+    }
 
     // block-table entries of this wavefront's pages: pairs wave, wave + 4, ...; lane 2 i + h holds page h of its pair i
     const int npages = (w.tok1 - w.tok0 + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE;   // <= 64 * kWaves
@@ -276,50 +441,70 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     const int npairs = (npages + 1) / 2;
     const int my_pairs = npairs > wave ? (npairs - wave + kWaves - 1) / kWaves : 0;
 
-    // Q as the B operand of S^T = K Q^T: lane (g, n) holds row n, the 8 dims that the lane's K holds (token-major and tiled
-    // bf16 pages: 32 kk + 8 g ..; 8-bit pages, 16 bytes of which are two operands: 64 (kk / 2) + 16 g + 8 (kk % 2) ..)
-    bf16x8 q[NT][KK];
     int limit[NT];   // last token that the lane's row sees
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = nt * 16 + n16;
-        const bool on = r < rows;
-        const int rr = w.row_lo + (on ? r : 0);
-        limit[nt] = on ? w.hide_from - 1 + (prefix ? 0 : rr / p.group) : -1;
-        const __bf16 *row = static_cast<const __bf16 *>(p.q) + (size_t)(w.row0 + rr / p.group) * p.q_stride + (size_t)(w.kvh * p.group + rr % p.group) * D;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-            q[nt][kk] = *reinterpret_cast<const bf16x8 *>(row + (B8 ? 64 * (kk / 2) + 16 * g + 8 * (kk % 2) : 32 * kk + 8 * g));
+        limit[nt] = r < rows ? w.hide_from - 1 + (prefix ? 0 : by_group(p, w.row_lo + r)) : -1;
     }
+    int q_at = 0;   // (0, but the compiler does not know: it would hold Q in registers throughout)
+    auto q_operand = [&](int nt, int kk) {
+        return *reinterpret_cast<const bf16x8 *>(sh.q + q_at + (nt * 16 + n16) * q_row_bytes(D) + (B8 ? 128 * (kk / 2) + 32 * g + 16 * (kk % 2) : 64 * kk + 16 * g));
+    };
 
     // Pages are read through descriptors that cover exactly one (page, KV head); a page that is not there has length 0,
     // for which the hardware returns zeros without touching memory.
     const char *khead = static_cast<const char *>(p.k_cache) + (size_t)w.kvh * kPageBytes;
     const char *vhead = static_cast<const char *>(p.v_cache) + (size_t)w.kvh * kPageBytes;
     const size_t page_stride = (size_t)p.Hkv * kPageBytes;
-    auto load = [&](int i, Pair<KIND, D> &r) {
+    Pair<KIND, D> cur;
+    auto page_of = [&](int i, int h, bool &valid) {
+        const int entry = __builtin_amdgcn_readlane(bt, i < my_pairs ? 2 * i + h : 0);
+        valid = i < my_pairs && entry >= 0;
+        return (size_t)(valid ? entry : 0);
+    };
+    auto load_k = [&](int i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int entry = __builtin_amdgcn_readlane(bt, i < my_pairs ? 2 * i + h : 0);
-            const bool valid = i < my_pairs && entry >= 0;
-            const size_t page = (size_t)(valid ? entry : 0);
-            const int bytes = valid ? kPageBytes : 0;
-            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + page * page_stride), 0, bytes, kBufferFlags);
-            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + page * page_stride), 0, bytes, kBufferFlags);
+            bool valid;
+            const size_t page = page_of(i, h, valid);
+            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + page * page_stride), 0, valid ? kPageBytes : 0, kBufferFlags);
 #pragma unroll
             for (int j = 0; j < Pair<KIND, D>::N; ++j)
-                r.k[h][j] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, j * 64, 0)
-                               : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, j * 1024, kStreamPolicy);
-#pragma unroll
-            for (int j = 0; j < Pair<KIND, D>::N; ++j) r.v[h][j] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, j * 1024, kStreamPolicy);
-            if constexpr (B8) {
-                const __amdgpu_buffer_rsrc_t sd = __builtin_amdgcn_make_buffer_rsrc(
-                    const_cast<float *>(p.kv_scale + (page * p.Hkv + w.kvh) * 32), 0, valid ? 128 : 0, kBufferFlags);
-                r.ks[h] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(sd, g * 16, 0, 0));
-                r.vs[h] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(sd, g * 16, 64, 0));
-            }
+                cur.k[h][j] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, j * 64, 0)
+                                 : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, j * 1024, kStreamPolicy);
         }
     };
+    auto load_scales = [&](int i) {
+        if constexpr (B8) {   // (no branch: a page that is not there is read as page 0, and not used)
+            bool valid;
+            const size_t page0 = page_of(i, 0, valid), page1 = page_of(i, 1, valid);
+            const float *at = p.kv_scale + (((n16 & 4) ? page1 : page0) * p.Hkv + w.kvh) * 32 + 4 * g + (n16 & 3);
+            cur.ks = at[0];
+            cur.vs = at[16];
+        }
+    };
+    auto load_v = [&](int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bool valid;
+            const size_t page = page_of(i, h, valid);
+            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + page * page_stride), 0, valid ? kPageBytes : 0, kBufferFlags);
+#pragma unroll
+            for (int j = 0; j < Pair<KIND, D>::N; ++j) cur.v[h][j] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, j * 1024, kStreamPolicy);
+        }
+    };
+    load_k(0);
+    load_scales(0);
+    load_v(0);
+    if (!place_partials(p, w)) return;
+#pragma unroll
+    for (int k = 0; k < QN; ++k) {
+        const int piece = k * kThreads + tid;
+        if (NT * 16 * QP % kThreads == 0 || piece < NT * 16 * QP)
+            *reinterpret_cast<u32x4 *>(sh.q + piece / QP * q_row_bytes(D) + piece % QP * 16) = q_piece[k];
+    }
+    __syncthreads();   // Q is in LDS
 
     f32x4 acc[NT][MT];
     float m_run[NT], l_run[NT];
@@ -331,9 +516,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    auto consume = [&](Pair<KIND, D> &cur, int i) {
+    // Each part of a pair's registers takes the next pair as soon as it has been used.
+    // (masked: some of the pair's tokens are hidden from some row, or past the end)
+    auto step = [&](int i, auto masked) {
+        constexpr bool need_mask = decltype(masked)::value;
         const int first = w.tok0 + 2 * (wave + kWaves * i) * SPEC_BLOCK_SIZE;
-        const bool need_mask = first + 2 * SPEC_BLOCK_SIZE > min(w.tok1, w.hide_from);
+        asm volatile("" : "+v"(q_at));   // (the query rows are read from LDS in every step, not kept in registers)
         // scores
         f32x4 s[NT][2];
 #pragma unroll
@@ -351,35 +539,41 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    s[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), q[nt][kk], s[nt][h], 0, 0, 0);
+                    s[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), q_operand(nt, kk), s[nt][h], 0, 0, 0);
             }
         }
-        // to base-2 exponents; per token: k = scale of x, lv = log2 of V's scale, rv = its reciprocal
+        load_k(i + 1);
+        // to base-2 exponents; per token: k = scale of x, lv = log2 of V's scale, rv = its reciprocal (each made by one lane of
+        // the row and handed to the others)
         f32x4 ks[2], lv[2], rv[2];
         if constexpr (B8) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float v = cur.vs[h][r] < kSmallestScale ? kSmallestScale : cur.vs[h][r];   // (a page that reads as zeros)
-                    ks[h][r] = cur.ks[h][r] * p.scale_log2;
-                    lv[h][r] = __builtin_amdgcn_logf(v);
-                    rv[h][r] = __builtin_amdgcn_rcpf(v);
-                }
+            bool there[2];
+            (void)page_of(i, 0, there[0]);
+            (void)page_of(i, 1, there[1]);
+            const bool on = (n16 & 4) ? there[1] : there[0];   // (a page that reads as zeros)
+            const float k1 = on ? cur.ks * p.scale_log2 : 0.0f, v1 = !on || cur.vs < kSmallestScale ? kSmallestScale : cur.vs;
+            const float l1 = __builtin_amdgcn_logf(v1), r1 = __builtin_amdgcn_rcpf(v1);
+            auto hand_out = [&](float x, f32x4(&to)[2]) {
+                to[0] = (f32x4){row_broadcast<0>(x), row_broadcast<1>(x), row_broadcast<2>(x), row_broadcast<3>(x)};
+                to[1] = (f32x4){row_broadcast<4>(x), row_broadcast<5>(x), row_broadcast<6>(x), row_broadcast<7>(x)};
+            };
+            hand_out(k1, ks);
+            hand_out(l1, lv);
+            hand_out(r1, rv);
         }
+        load_scales(i + 1);
         Weights pw[NT][TERMS];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float mx = -INFINITY;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[nt][h][r] = B8 ? fmaf(s[nt][h][r], ks[h][r], lv[h][r]) : s[nt][h][r] * p.scale_log2;
                     if (need_mask && first + h * SPEC_BLOCK_SIZE + 4 * g + r > min(limit[nt], w.tok1 - 1)) s[nt][h][r] = -INFINITY;
-                    mx = fmaxf(mx, s[nt][h][r]);
                 }
             }
+            float mx = max3(max3(s[nt][0][0], s[nt][0][1], s[nt][0][2]), max3(s[nt][0][3], s[nt][1][0], s[nt][1][1]), __builtin_elementwise_maximum(s[nt][1][2], s[nt][1][3]));
             mx -= kTop;
             const float most = m_run[nt] + kRescaleSlack;
             if (__builtin_amdgcn_ballot_w64(mx > most) != 0) {
@@ -515,78 +709,105 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                         acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[mt]), __builtin_bit_cast(bf16x8, pw[nt][t]), acc[nt][mt], 0, 0, 0);
             }
         }
+        load_v(i + 1);
     };
 
-    {
-        Pair<KIND, D> a, b;
-        load(0, a);
-        for (int i = 0; i < my_pairs; i += 2) {
-            load(i + 1, b);
-            consume(a, i);
-            load(i + 2, a);
-            if (i + 1 < my_pairs) consume(b, i + 1);
-        }
-    }
+    const int all_see = min(w.tok1, w.hide_from) - w.tok0;   // tokens that every row sees
+    const int plain = min(my_pairs, all_see / (2 * SPEC_BLOCK_SIZE) > wave ? (all_see / (2 * SPEC_BLOCK_SIZE) - wave + kWaves - 1) / kWaves : 0);
+    int i = 0;
+    for (; i < plain; ++i) step(i, std::false_type());
+    for (; i < my_pairs; ++i) step(i, std::true_type());
 
-    // merge the wavefronts: 2, 3 into 0, 1, then 1 into 0
+    // Merge the wavefronts: each takes a quarter of the head dims of all rows and finds the others' results for them in LDS.
+    constexpr int SN = Shared<KIND, NT, D>::kSlices;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) l_run[nt] = sum_across_rows(l_run[nt]);
-    auto put = [&](int buf) {
+    __syncthreads();   // (the walk's regions are free)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) sh.acc[buf][nt][mt][lane] = acc[nt][mt];
-            sh.m[buf][nt][lane] = m_run[nt];
-            sh.l[buf][nt][lane] = l_run[nt];
+    for (int nt = 0; nt < NT; ++nt) {
+        if (g == 0) {
+            sh.m[wave][nt][n16] = m_run[nt];
+            sh.l[wave][nt][n16] = l_run[nt];
         }
-    };
-    auto merge = [&](int buf) {
+    }
+    RowSum<SN> sum[NT];   // row nt * 16 + n16, dims (wave * SN + i) * 16 + 4 g .. + 3
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float mo = sh.m[buf][nt][lane], mn = fmaxf(m_run[nt], mo);
-            const float wa = fast_exp2(m_run[nt] - mn), wb = fast_exp2(mo - mn);
-            l_run[nt] = l_run[nt] * wa + sh.l[buf][nt][lane] * wb;
-            m_run[nt] = mn;
+    for (int to = 0; to < kWaves; ++to) {
+        if (to == wave) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = acc[nt][mt] * wa + sh.acc[buf][nt][mt][lane] * wb;
-        }
-    };
-    __syncthreads();   // (the regions of the walk are free)
-    if (wave >= 2) put(wave - 2);
-    __syncthreads();
-    if (wave < 2) merge(wave);
-    __syncthreads();
-    if (wave == 1) put(0);
-    __syncthreads();
-    if (wave == 0) {
-        merge(0);   // (its reads precede the writes below in program order)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+                for (int i = 0; i < SN; ++i) sum[nt].o[i] = acc[nt][to * SN + i];
+        } else {
+            const int from = wave - (wave > to ? 1 : 0);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                *reinterpret_cast<f32x4 *>(sh.o + (nt * 16 + n16) * o_row_bytes(D) + (mt * 16 + 4 * g) * 4) = acc[nt][mt];
-            if (g == 0) {
-                sh.row_m[nt * 16 + n16] = m_run[nt];
-                sh.row_l[nt * 16 + n16] = l_run[nt];
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < SN; ++i) sh.acc[to][from][nt][i][lane] = acc[nt][to * SN + i];
         }
     }
     __syncthreads();
-
-    constexpr int OP = D / 4;   // pieces of four dims in a row
-    if (prefix || w.nchunks > 1) {
-        float *const acc_out = prefix ? p.prefix_acc : p.acc, *const ml_out = prefix ? p.prefix_ml : p.ml;
-        const int chunks = prefix ? p.max_prefix_chunks : p.max_chunks;
-        for (int piece = tid; piece < rows * OP; piece += kThreads) {
-            const int r = piece / OP, c = piece % OP;
-            const size_t slot = out_index(r) * chunks + w.chunk;
-            const f32x4 o = *reinterpret_cast<const f32x4 *>(sh.o + r * o_row_bytes(D) + c * 16);
-            unsigned long long *dst = reinterpret_cast<unsigned long long *>(acc_out + slot * D + c * 4);
-            publish_u64(dst, pack_f32x2(o[0], o[1]));
-            publish_u64(dst + 1, pack_f32x2(o[2], o[3]));
-            if (c == 0) publish_u64(reinterpret_cast<unsigned long long *>(ml_out + slot * 2), pack_f32x2(sh.row_m[r], sh.row_l[r]));
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        float m[kWaves], top = m_run[nt];
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            m[k] = sh.m[k][nt][n16];
+            top = fmaxf(top, m[k]);
         }
-        if (prefix) return;
+        const float own = fast_exp2(m_run[nt] - top);
+        sum[nt].m = top;
+        sum[nt].l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SN; ++i) sum[nt].o[i] *= own;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) sum[nt].l = fmaf(sh.l[k][nt][n16], fast_exp2(m[k] - top), sum[nt].l);
+#pragma unroll
+        for (int k = 0; k < kWaves - 1; ++k) {
+            const float take = fast_exp2((k < wave ? m[k] : m[k + 1]) - top);
+#pragma unroll
+            for (int i = 0; i < SN; ++i) sum[nt].o[i] += sh.acc[wave][k][nt][i][lane] * take;
+        }
+    }
+
+    size_t rh[NT];   // packed (token row, query head) of the lane's rows (past the last: the last one's, not written)
+    bool on[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 16 + n16;
+        on[nt] = r < rows;
+        rh[nt] = packed_row(p, w.row0, w.kvh, w.row_lo + min(r, rows - 1));
+    }
+    const int dim0 = wave * (SN * 16) + 4 * g;
+    if (prefix) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (!on[nt]) continue;
+            const size_t slot = rh[nt] * p.max_prefix_chunks + w.chunk;
+#pragma unroll
+            for (int i = 0; i < SN; ++i) *reinterpret_cast<f32x4 *>(p.prefix_acc + slot * D + dim0 + i * 16) = sum[nt].o[i];
+            if (wave == 0 && g == 0) *reinterpret_cast<f32x2 *>(p.prefix_ml + slot * 2) = (f32x2){sum[nt].m, sum[nt].l};
+        }
+        return;
+    }
+    if (w.nchunks > 1) {
+        // Partial results go from block to block inside the launch: past the cache levels that are not coherent
+        // (kDeviceScope), 16 bytes at a time through descriptors of the request's part of the workspace.
+        const size_t part = (size_t)w.row0 * p.Hq * p.max_chunks;
+        const __amdgpu_buffer_rsrc_t acc_d = __builtin_amdgcn_make_buffer_rsrc(p.acc + part * D, 0, 0xFFFFFFFFu, kBufferFlags);
+        const __amdgpu_buffer_rsrc_t ml_d = __builtin_amdgcn_make_buffer_rsrc(p.ml + part * 2, 0, 0xFFFFFFFFu, kBufferFlags);
+        uint32_t at[NT];   // the row's first slot in it
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) at[nt] = (uint32_t)(rh[nt] - (size_t)w.row0 * p.Hq) * (uint32_t)p.max_chunks;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (!on[nt]) continue;
+#pragma unroll
+            for (int i = 0; i < SN; ++i)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sum[nt].o[i]), acc_d, ((at[nt] + w.chunk) * D + dim0 + i * 16) * 4, 0, kDeviceScope);
+            if (wave == 0 && g == 0)
+                __builtin_amdgcn_raw_buffer_store_b64((u32x2){__float_as_uint(sum[nt].m), __float_as_uint(sum[nt].l)}, ml_d, (at[nt] + w.chunk) * 8, 0, kDeviceScope);
+        }
         writes_complete();   // the partials are in memory before the ticket is taken
         __syncthreads();
         if (tid == 0) {
@@ -598,35 +819,450 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         __syncthreads();
         if (!sh.last) return;
         order_after_ticket();
+        // the last chunk to finish: all of them in chunk order, a few of all rows on their way together
+        constexpr int U = NT <= 2 ? 4 : 2;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sum[nt].clear();
+        for (int c0 = 0; c0 < w.nchunks; c0 += U) {
+            u32x2 ml[NT][U];
+            u32x4 o[NT][U][SN];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t slot = at[nt] + min(c0 + u, w.nchunks - 1);
+                    ml[nt][u] = __builtin_amdgcn_raw_buffer_load_b64(ml_d, slot * 8, 0, kDeviceScope);
+#pragma unroll
+                    for (int i = 0; i < SN; ++i) o[nt][u][i] = __builtin_amdgcn_raw_buffer_load_b128(acc_d, (slot * D + dim0 + i * 16) * 4, 0, kDeviceScope);
+                }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    f32x4 x[SN];
+#pragma unroll
+                    for (int i = 0; i < SN; ++i) x[i] = __builtin_bit_cast(f32x4, o[nt][u][i]);
+                    if (c0 + u < w.nchunks) sum[nt].add(__uint_as_float(ml[nt][u].x), __uint_as_float(ml[nt][u].y), x);
+                }
+        }
     }
-    // the rows' results: the prefix's partials, then the own ones in chunk order
-    for (int piece = tid; piece < rows * OP; piece += kThreads) {
-        const int r = piece / OP, c = piece % OP;
-        const size_t rh = out_index(r);
-        RowSum sum;
-        add_prefix<D>(p, sum, rh, w.prefix_chunks, c * 4);
-        if (w.nchunks == 1) {
-            sum.add(sh.row_m[r], sh.row_l[r], *reinterpret_cast<const f32x4 *>(sh.o + r * o_row_bytes(D) + c * 16));
+    // the prefix's partial results: a row's are those of the blocks from the one that took the first step of its row block to the
+    // one that took the last (many rows), or one of each chunk
+    int pieces[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        pieces[nt] = w.prefix_chunks;
+        if (w.prefix_pairs > 0) {
+            const int rr = (w.row0 - w.prefix_row0) * p.group + w.row_lo + min(nt * 16 + n16, rows - 1);
+            const int step = w.prefix_base + rr / kPrefixRows * w.prefix_pairs;
+            pieces[nt] = (step + w.prefix_pairs - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
+        }
+    }
+    if (w.prefix > 0) {
+        constexpr int U = NT <= 2 ? 4 : 2;
+        int most = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) most = max(most, pieces[nt]);
+        for (int c0 = 0; __builtin_amdgcn_ballot_w64(c0 < most) != 0; c0 += U) {
+            f32x2 ml[NT][U];
+            f32x4 o[NT][U][SN];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, pieces[nt] - 1);
+                    ml[nt][u] = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
+#pragma unroll
+                    for (int i = 0; i < SN; ++i) {
+                        const size_t from = slot * D + dim0 + i * 16;
+                        if (!FULL && w.prefix_pairs > 0)
+                            o[nt][u][i] = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(reinterpret_cast<const _Float16 *>(p.prefix_acc) + from), f32x4);
+                        else
+                            o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + from);
+                    }
+                }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u < pieces[nt]) sum[nt].add(ml[nt][u].x, ml[nt][u].y, o[nt][u]);
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        if (!on[nt]) continue;
+        const float inv = sum[nt].l == 0.0f ? 0.0f : 1.0f / sum[nt].l;   // (a row that has seen no key is zero)
+#pragma unroll
+        for (int i = 0; i < SN; ++i) {
+            const f32x4 o = sum[nt].o[i] * inv;
+            if (p.out_f32)
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + rh[nt] * D + dim0 + i * 16) = o;
+            else
+                *reinterpret_cast<u32x2 *>(static_cast<__bf16 *>(p.out) + rh[nt] * D + dim0 + i * 16) =
+                    __builtin_bit_cast(u32x2, __builtin_convertvector(o, bf16x4));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Prefixes of groups with many query rows.
+//
+// The work is counted in (row block of 128 rows, pair of pages) steps, laid out KV head by KV head, group by group, row block
+// by row block; every block takes the same number of consecutive steps, whatever row blocks they belong to, and leaves a
+// partial result for each row block it touches.  So all blocks end together however ragged the groups are, and the blocks
+// of an XCD share their KV heads' pages in its L2.
+//
+// A block's four wavefronts have 32 rows each and walk the same pages, which pass through LDS once for all of them, a pair
+// of pages (32 tokens) at a time.  In LDS a pair lies as the operands of v_mfma_f32_32x32x16 want it, 16 bytes per lane
+// and 1 KB per read, as 16-bit values whatever the cache holds (8-bit codes are converted once on the way in);
+// token-major V is stored by rows and read through the transposing read.  (lane = 32 half + c)
+//   S^T[token][row] = K[token][:] . Q[row][:]: 16 dims per instruction, lane (half, c) holds row c, tokens
+//   4 half + 8 i + 0..3, i = 0, 1 of the first page, 2, 3 of the second
+//   O^T[dim][row] += V^T[dim][token] . P^T[token][row]: a page per instruction, its tokens in that order
+// Two LDS buffers and one barrier per pair.  Blocks of a compute unit are not in step with each other, and that is what
+// keeps its matrix cores and its vector units busy at the same time.
+// ---------------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <int KIND, int D>
+struct RowsShared {
+    static constexpr int kK = 2 * SPEC_BLOCK_SIZE * D * 2;   // of a pair
+    static constexpr int kV = 2 * SPEC_BLOCK_SIZE * (KIND == kCacheTokens ? v_row_bytes(D) : D * 2);
+    static constexpr int kOutRow = D * 2 + 16;               // half a result row
+    union {
+        struct {
+            alignas(16) unsigned char k[2][kK];   // [16-dim step][lane][16]
+            alignas(16) unsigned char v[2][kV];   // [page][32-dim slice][lane][tokens 4 half .. + 3, 8 + 4 half .. + 3]; token-major: [page][token] rows
+        };
+        alignas(16) unsigned char o[kWaves][32 * kOutRow];   // results on their way out, by half rows
+    };
+    // 8-bit pages, per token: K's scale with the softmax scale, log2 of V's, its reciprocal
+    float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? 2 * SPEC_BLOCK_SIZE : 1];
+    int page[2 * kMaxPrefixPairs + 8];   // (one for each thread, and four more pairs)
+    static_assert(2 * kMaxPrefixPairs == kThreads, "a thread per page");   // the steps' block-table entries; -1: outside the pool, or past the end
+};
+
+template <int KIND, int D, bool FULL>
+__global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParams p)
+{
+    constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;
+    constexpr int KS = D / 16, SL = D / 32;
+    constexpr int kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);
+    constexpr int N = B8 ? D / 64 : D / 32;              // 1 KB pieces of a page's K, of its V
+    constexpr int PN = N >= 2 ? N / 2 : 1;               // ... that a wavefront brings in
+    constexpr int TERMS = FULL ? (B8 ? 2 : 3) : 1;
+    constexpr float kTop = B8 ? 7.0f : 0.0f;
+    typedef std::conditional_t<B8, f16x8, bf16x8> Weights;
+    typedef RowsShared<KIND, D> Sh;
+    __shared__ Sh sh;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, c32 = lane & 31, n16 = lane & 15, g = lane >> 4;
+    // consecutive blocks go to different XCDs; consecutive steps stay on one
+    const int block = (int)(blockIdx.x % kXcdCount) * (gridDim.x / kXcdCount) + blockIdx.x / kXcdCount;
+
+    GroupLanes groups;
+    groups.look(p, 0);
+    int total = groups.total();   // steps of a KV head
+    if (p.G > kWave) prefix_steps(p, -1, total);
+    if ((int64_t)total * p.Hkv > (int64_t)gridDim.x * p.prefix_block_steps) return;   // (not the groups planned for: the own launch reports it)
+    int pos = block * p.prefix_block_steps;
+    const int end = min(pos + p.prefix_block_steps, total * p.Hkv);
+
+    while (pos < end) {
+        // the row block that step `pos` belongs to
+        const int kvh = pos / total;
+        PrefixPlace at = {};
+        int step = pos - kvh * total;
+        if (p.G <= kWave) {
+            groups.find(step, at);
         } else {
-#pragma unroll 4
-            for (int k = 0; k < w.nchunks; ++k) {
-                const size_t slot = rh * p.max_chunks + k;
-                const unsigned long long *src = reinterpret_cast<const unsigned long long *>(p.acc + slot * D + c * 4);
-                const unsigned long long ml = fetch_u64(reinterpret_cast<const unsigned long long *>(p.ml + slot * 2));
-                const unsigned long long o0 = fetch_u64(src), o1 = fetch_u64(src + 1);
-                sum.add(__uint_as_float((uint32_t)ml), __uint_as_float((uint32_t)(ml >> 32)),
-                        (f32x4){__uint_as_float((uint32_t)o0), __uint_as_float((uint32_t)(o0 >> 32)), __uint_as_float((uint32_t)o1),
-                                __uint_as_float((uint32_t)(o1 >> 32))});
+            for (int base = 0; base < p.G; base += kWave) {
+                groups.look(p, base);
+                if (groups.find(step, at)) break;
+                step -= groups.total();
             }
         }
-        write_row<D>(p, rh, c * 4, sum);
+        const int pairs = min(at.pairs - at.first, end - pos);
+        const int slot = block - (pos - at.first) / p.prefix_block_steps;
+        const int row0 = at.row0;                                   // the group's first packed token row
+        const int row_lo = at.row_block * kPrefixRows + wave * 32;
+        const int rows = min(max(at.rows - row_lo, 0), 32);         // this wavefront's
+        auto out_index = [&](int r) {
+            return packed_row(p, row0, kvh, row_lo + r);
+        };
+        __syncthreads();   // (the previous row block's results have left LDS)
+        const int last_pages = at.pages - 2 * (at.first + pairs - 1);   // of the last pair: 1 or 2 (or more follow)
+        bf16x8 q[KS];
+        {
+            const __bf16 *row = query_row(p, row0, kvh, c32 < rows ? row_lo + c32 : 0);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(row + 16 * ks + 8 * half);
+        }
+        {
+            const int have = at.pages - 2 * at.first;               // pages from the first one of these steps on
+            const bool used = tid < 2 * pairs && tid < have;
+            int entry = -1;
+            if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + 2 * at.first + tid];
+            const bool bad = used && (unsigned)entry >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
+            sh.page[tid] = bad ? -1 : entry;
+            if (tid < 8) sh.page[2 * kMaxPrefixPairs + tid] = -1;
+            const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
+            if (bad_lanes != 0 && kvh == 0 && at.row_block == 0 && lane == 0 && p.errors != nullptr)
+                atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
+        }
+        __syncthreads();
+
+        // Wavefront w brings in pieces w / 2, w / 2 + 2 of K and of V of page w % 2.
+        const int my_page = wave & 1, j0 = wave >> 1;
+        const char *khead = static_cast<const char *>(p.k_cache) + (size_t)kvh * kPageBytes;
+        const char *vhead = static_cast<const char *>(p.v_cache) + (size_t)kvh * kPageBytes;
+        const size_t page_stride = (size_t)p.Hkv * kPageBytes;
+        struct {
+            u32x4 k[PN], v[PN];
+            float scale;   // 8-bit, wavefronts 0 and 1: the page's record, an entry per lane
+        } in;
+        auto load = [&](int u) {
+            if (N == 1 && wave >= 2) return;   // (two pieces in all)
+            const int entry = __builtin_amdgcn_readfirstlane(sh.page[2 * u + my_page]);
+            const bool valid = entry >= 0;
+            const size_t page = (size_t)(valid ? entry : 0);
+            const int bytes = valid ? kPageBytes : 0;
+            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + page * page_stride), 0, bytes, kBufferFlags);
+            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + page * page_stride), 0, bytes, kBufferFlags);
+#pragma unroll
+            for (int i = 0; i < PN; ++i) {
+                in.k[i] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, (j0 + 2 * i) * 64, 0)
+                             : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, (j0 + 2 * i) * 1024, 0);
+                in.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, (j0 + 2 * i) * 1024, 0);
+            }
+            if constexpr (B8) {
+                const __amdgpu_buffer_rsrc_t sd = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<float *>(p.kv_scale + (page * p.Hkv + kvh) * 32), 0, valid ? 128 : 0, kBufferFlags);
+                in.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sd, c32 * 4, 0, 0));
+            }
+        };
+        auto store = [&](int buf) {
+            if (N == 1 && wave >= 2) return;
+            unsigned char *ks = sh.k[buf], *vs = sh.v[buf];
+#pragma unroll
+            for (int i = 0; i < PN; ++i) {
+                const int j = j0 + 2 * i;
+                if constexpr (B8) {   // token n16, dims 64 j + 16 g .. + 15; tokens 4 g .. + 3, dims 64 j + 16 e + n16
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const u32x2 a = codes_to_bf16<INT8>(in.k[i][2 * e]), b = codes_to_bf16<INT8>(in.k[i][2 * e + 1]);
+                        *reinterpret_cast<u32x4 *>(ks + (4 * j + g) * 1024 + (e * 32 + my_page * 16 + n16) * 16) = (u32x4){a.x, a.y, b.x, b.y};
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<u32x2 *>(vs + (my_page * SL + 2 * j + e / 2) * 1024 + ((g & 1) * 32 + (e % 2) * 16 + n16) * 16 + (g >> 1) * 8) =
+                            codes_to_f16<INT8>(in.v[i][e]);
+                } else {              // token n16, dims 32 j + 8 g .. + 7
+                    *reinterpret_cast<u32x4 *>(ks + (2 * j + (g >> 1)) * 1024 + ((g & 1) * 32 + my_page * 16 + n16) * 16) = in.k[i];
+                    if constexpr (TM) {
+                        constexpr int LR = D / 8;   // lanes per token row of a 1 KB load
+                        *reinterpret_cast<u32x4 *>(vs + (my_page * SPEC_BLOCK_SIZE + (kWave / LR) * j + lane / LR) * v_row_bytes(D) + (lane % LR) * 16) = in.v[i];
+                    } else {          // tokens 4 g .. + 3, dims 32 j + 16 e + n16
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            *reinterpret_cast<u32x2 *>(vs + (my_page * SL + j) * 1024 + ((g & 1) * 32 + e * 16 + n16) * 16 + (g >> 1) * 8) =
+                                (u32x2){in.v[i][2 * e], in.v[i][2 * e + 1]};
+                    }
+                }
+            }
+            if constexpr (B8) {
+                if (wave < 2 && lane < 32) {
+                    if (lane < 16) {
+                        sh.scale[buf][0][my_page * 16 + lane] = in.scale * p.scale_log2;
+                    } else {
+                        const float x = in.scale < kSmallestScale ? kSmallestScale : in.scale;   // (a page that reads as zeros)
+                        sh.scale[buf][1][my_page * 16 + lane - 16] = __builtin_amdgcn_logf(x);
+                        sh.scale[buf][2][my_page * 16 + lane - 16] = __builtin_amdgcn_rcpf(x);
+                    }
+                }
+            }
+        };
+
+        f32x16 acc[SL];
+        float m_run = kEmptyMax, l_run = 0.0f;
+#pragma unroll
+        for (int sl = 0; sl < SL; ++sl)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[sl][e] = 0.0f;
+
+        f32x16 s;
+        Weights pw[2][TERMS];
+        // products of the K in buffer `buf` with the queries
+        auto scores = [&](int buf) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(sh.k[buf] + ks * 1024 + lane * 16), q[ks], s, 0, 0, 0);
+        };
+        // scores to base-2 exponents (8-bit; bf16: up to the scale, which the exponent's multiply-add applies); the running reference
+        // raised where it has fallen behind; weights
+        auto weigh = [&](int buf, bool one_page) {
+            if constexpr (B8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 ks = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][0][8 * i + 4 * half]);
+                    const f32x4 lv = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][1][8 * i + 4 * half]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[4 * i + r] = fmaf(s[4 * i + r], ks[r], lv[r]);
+                }
+            }
+            if (one_page) {
+#pragma unroll
+                for (int e = 8; e < 16; ++e) s[e] = -INFINITY;
+            }
+            float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]);
+            a = max3(a, s[6], s[7]);
+            b = max3(b, s[8], s[9]);
+            a = max3(a, s[10], s[11]);
+            b = max3(b, s[12], s[13]);
+            a = max3(a, s[14], s[15]);
+            float mx = max3(a, b, b);
+            mx = B8 ? mx - kTop : mx * p.scale_log2;   // (the scale is positive: the maximum commutes with it)
+            const float limit = m_run + kRescaleSlack;
+            if (__builtin_amdgcn_ballot_w64(mx > limit) != 0) {
+                mx = max_across_xor32(mx);
+                const float m_new = mx > limit ? mx : m_run;
+                const float alpha = fast_exp2(m_run - m_new);
+                l_run *= alpha;
+#pragma unroll
+                for (int sl = 0; sl < SL; ++sl) acc[sl] *= alpha;
+                m_run = m_new;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x4 rv = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (B8) rv = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][2][8 * i + 4 * half]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = s[4 * i + r];
+                    const float e = fast_exp2(B8 ? x - m_run : fmaf(x, p.scale_log2, -m_run));
+                    if constexpr (B8) l_run = fmaf(e, rv[r], l_run);
+                    else if constexpr (FULL) l_run += e;
+                    float rest = e;
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) {
+                        pw[i / 2][t][4 * (i % 2) + r] = (std::conditional_t<B8, _Float16, __bf16>)rest;
+                        rest -= (float)pw[i / 2][t][4 * (i % 2) + r];
+                    }
+                }
+            }
+            if constexpr (!B8 && !FULL) {   // the sum of the weights as they are multiplied, two at a time
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        l_run = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pw[h][0][e], pw[h][0][e + 1]}, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, l_run, false);
+            }
+        };
+        // the weights' product with the V in buffer `buf`
+        auto product = [&](int buf) {
+            const unsigned char *v0 = sh.v[buf];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int sl = 0; sl < SL; ++sl) {
+                    u32x4 v;
+                    if constexpr (TM) {
+                        const unsigned char *src = v0 + (h * SPEC_BLOCK_SIZE + 4 * half + (n16 >> 2)) * v_row_bytes(D) + (32 * sl + 16 * (g & 1) + 4 * (n16 & 3)) * 2;
+                        const u32x2 a = read_transposed(src), b = read_transposed(src + 8 * v_row_bytes(D));
+                        v = (u32x4){a.x, a.y, b.x, b.y};
+                    } else {
+                        v = *reinterpret_cast<const u32x4 *>(v0 + (h * SL + sl) * 1024 + lane * 16);
+                    }
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) {
+                        if constexpr (B8) acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pw[h][t]), acc[sl], 0, 0, 0);
+                        else acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pw[h][t]), acc[sl], 0, 0, 0);
+                    }
+                }
+        };
+
+        load(0);
+        store(0);
+        load(1);
+        for (int u = 0; u < pairs; ++u) {
+            __syncthreads();        // pair u is in LDS, and no wavefront reads pair u - 1 any more
+            store((u + 1) & 1);
+            load(u + 2);
+            scores(u & 1);
+            weigh(u & 1, u == pairs - 1 && last_pages == 1);
+            product(u & 1);
+        }
+
+        // The rows' partial results, half of the dims at a time through LDS so that they go out in long pieces.
+        l_run += __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false)[half ^ 1]);
+        if constexpr (!FULL) {
+            // As fp16, whose rounding (2^-12 of a value, or of 2^-14 of the row's largest) is small beside that of the bf16
+            // output: half the bytes to write here and to read back.  The row's reference takes the power of two that
+            // brings its largest finite value to at most one.
+            float most = 0.0f;
+#pragma unroll
+            for (int sl = 0; sl < SL; ++sl)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float x = __builtin_fabsf(acc[sl][e]);
+                    most = x < INFINITY && x > most ? x : most;
+                }
+            most = max_across_xor32(most);
+            const int up = __builtin_amdgcn_frexp_expf(most);
+            m_run += (float)up;
+            l_run = __builtin_amdgcn_ldexpf(l_run, -up);
+#pragma unroll
+            for (int sl = 0; sl < SL; ++sl)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[sl][e] = __builtin_amdgcn_ldexpf(acc[sl][e], -up);
+        }
+        if (half == 0 && c32 < rows)
+            *reinterpret_cast<f32x2 *>(p.prefix_ml + (out_index(c32) * p.max_prefix_chunks + slot) * 2) = (f32x2){m_run, l_run};
+        __syncthreads();
+        unsigned char *o = sh.o[wave];
+        constexpr int kPartial = FULL ? 4 : 2;        // bytes of a value
+        constexpr int OP = D / 2 * kPartial / 16;     // 16-byte pieces of half a row
+#pragma unroll
+        for (int d2 = 0; d2 < 2; ++d2) {   // (a region for each wavefront, and LDS executes a wavefront's accesses in order)
+#pragma unroll
+            for (int sl = 0; sl < SL / 2; ++sl)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x16 &x = acc[d2 * (SL / 2) + sl];
+                    const f32x4 four = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+                    unsigned char *at4 = o + c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * half) * kPartial;
+                    if constexpr (FULL) *reinterpret_cast<f32x4 *>(at4) = four;
+                    else *reinterpret_cast<f16x4 *>(at4) = __builtin_convertvector(four, f16x4);
+                }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int piece = lane; piece < 32 * OP; piece += kWave) {
+                const int r = piece / OP, c = piece % OP;
+                if (r < rows)
+                    *reinterpret_cast<u32x4 *>(reinterpret_cast<unsigned char *>(p.prefix_acc) +
+                                               ((out_index(r) * p.max_prefix_chunks + slot) * D + d2 * (D / 2)) * kPartial + c * 16) =
+                        *reinterpret_cast<const u32x4 *>(o + r * Sh::kOutRow + c * 16);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        pos += pairs;
     }
 }
 
 template <int KIND, int NT, int D, bool FULL>
 void go(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
 {
-    hipLaunchKernelGGL((cache_attn_kernel<KIND, NT, D, FULL>), dim3(at.blocks), dim3(kThreads), 0, stream, p, at.prefix);
+    if (at.many_rows) {
+        if constexpr (NT == 1) hipLaunchKernelGGL((prefix_rows_kernel<KIND, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p);
+        return;
+    }
+    hipLaunchKernelGGL((cache_attn_kernel<KIND, NT, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p, at.prefix);
 }
 
 }  // namespace
@@ -668,11 +1304,11 @@ hipError_t launch_kind(const CacheAttnParams &p, int tiles, CacheLaunch at, hipS
 hipError_t launch_cache_attn(const CacheAttnParams &p, hipStream_t stream)
 {
     if (p.max_prefix_chunks > 0) {
-        const unsigned blocks = (unsigned)(p.prefix_row_blocks * p.Hkv * p.max_prefix_chunks);
-        const hipError_t err = launch_kind(p, p.prefix_tiles, CacheLaunch{blocks, 1}, stream);
+        const dim3 blocks = p.prefix_many_rows ? dim3(p.prefix_row_blocks) : dim3(p.Hkv, p.prefix_row_blocks, p.max_prefix_chunks);
+        const hipError_t err = launch_kind(p, p.prefix_many_rows ? 1 : p.prefix_tiles, CacheLaunch{blocks, 1, p.prefix_many_rows}, stream);
         if (err != hipSuccess) return err;
     }
-    return launch_kind(p, p.row_tiles, CacheLaunch{(unsigned)(p.row_blocks * p.B * p.Hkv * p.max_chunks), 0}, stream);
+    return launch_kind(p, p.row_tiles, CacheLaunch{dim3(p.Hkv, p.B, p.row_blocks * p.max_chunks), 0, 0}, stream);
 }
 
 #endif

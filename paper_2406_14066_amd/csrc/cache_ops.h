@@ -47,7 +47,11 @@ hipError_t launch_kv8_read(const Kv8ReadParams &p, hipStream_t stream);
 //            partials in and writes the output; otherwise the last of its blocks to finish merges all partials (tickets).
 // Partial results of query row r (token row * Hq + head), chunk c:
 //   acc [r][max chunks][d]  sum_t 2^(x_t - m) V_t, un-normalised    ml [r][max chunks][2]  m and sum_t 2^(x_t - m)
+// in fp32 (prefixes with many rows and a bf16 output: acc in fp16).
 constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's four wavefronts: 64 pages each
+
+constexpr int kPrefixRows = 128;        // many rows: rows of a row block
+constexpr int kMaxPrefixPairs = 128;    // ... and most steps (pairs of pages) of a block
 
 struct CacheAttnParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, G;
@@ -57,9 +61,11 @@ struct CacheAttnParams {
     int32_t capacity_tokens;                    // longest kv_len planned for
     int32_t prefix_tiles, prefix_row_blocks;    // prefix: 16-row tiles of a block, blocks over all groups
     int32_t prefix_chunk_tokens, max_prefix_chunks;   // 0: no group has a prefix
+    int32_t prefix_many_rows, prefix_block_steps;   // the launch for many rows: steps of a block, prefix_row_blocks blocks
     int32_t prefix_capacity;                    // longest prefix planned for
     int32_t max_q_rows;                         // rows of the largest request
     uint32_t generation;
+    uint32_t group_inverse;                     // 2^32 / group, rounded up
     float scale_log2;
     int64_t q_stride;                           // elements per token
     const void *q, *k_cache, *v_cache;
