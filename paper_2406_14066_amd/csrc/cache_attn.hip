@@ -41,6 +41,15 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kDeviceScope = 16;        // "sc1" bit of a raw buffer access: coherent over the device's caches
 constexpr float kRescaleSlack = 8.0f;   // the running reference follows the maximum when it is this much behind
 
+// Partial results of the launch for many rows keep a row's dims in the order in which the wavefronts that merge them hold
+// them: four groups of 4 from each 16-dim slice of a wavefront (D = 128: two slices), a lane's dims side by side.
+template <int D>
+__device__ __forceinline__ constexpr int partial_place(int dim)   // of four dims
+{
+    if constexpr (D == 128) return dim / 32 * 32 + dim % 16 / 4 * 8 + dim % 32 / 16 * 4;
+    return dim;
+}
+
 constexpr int v_row_bytes(int D) { return D * 2 + 16; }   // token rows of V in LDS (token-major pages)
 constexpr int q_row_bytes(int D) { return D * 2 + 16; }   // query rows in LDS
 
@@ -498,6 +507,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     load_scales(0);
     load_v(0);
     if (!place_partials(p, w)) return;
+    // Partial results of the block's row r: those of the blocks from the one that took the first step of its row block to the one that
+    // took the last (many rows), or one of each chunk.
+    auto partials_of = [&](int r) {
+        if (w.prefix_pairs == 0) return w.prefix_chunks;
+        const int rr = (w.row0 - w.prefix_row0) * p.group + w.row_lo + r;
+        const int step = w.prefix_base + rr / kPrefixRows * w.prefix_pairs;
+        return (step + w.prefix_pairs - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
+    };
 #pragma unroll
     for (int k = 0; k < QN; ++k) {
         const int piece = k * kThreads + tid;
@@ -846,18 +863,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                 }
         }
     }
-    // the prefix's partial results: a row's are those of the blocks from the one that took the first step of its row block to the
-    // one that took the last (many rows), or one of each chunk
+    // the prefix's partial results
     int pieces[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        pieces[nt] = w.prefix_chunks;
-        if (w.prefix_pairs > 0) {
-            const int rr = (w.row0 - w.prefix_row0) * p.group + w.row_lo + min(nt * 16 + n16, rows - 1);
-            const int step = w.prefix_base + rr / kPrefixRows * w.prefix_pairs;
-            pieces[nt] = (step + w.prefix_pairs - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
-        }
-    }
+    for (int nt = 0; nt < NT; ++nt) pieces[nt] = partials_of(min(nt * 16 + n16, rows - 1));
     if (w.prefix > 0) {
         constexpr int U = NT <= 2 ? 4 : 2;
         int most = 0;
@@ -872,13 +881,20 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                 for (int u = 0; u < U; ++u) {
                     const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, pieces[nt] - 1);
                     ml[nt][u] = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
+                    if (w.prefix_pairs > 0) {   // (see partial_place)
+                        const size_t from = slot * D + wave * (SN * 16) + g * (SN * 4);
+                        if constexpr (!FULL) {
+                            typedef _Float16 Halves __attribute__((ext_vector_type(4 * SN)));
+                            const Halves x = *reinterpret_cast<const Halves *>(reinterpret_cast<const _Float16 *>(p.prefix_acc) + from);
 #pragma unroll
-                    for (int i = 0; i < SN; ++i) {
-                        const size_t from = slot * D + dim0 + i * 16;
-                        if (!FULL && w.prefix_pairs > 0)
-                            o[nt][u][i] = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(reinterpret_cast<const _Float16 *>(p.prefix_acc) + from), f32x4);
-                        else
-                            o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + from);
+                            for (int i = 0; i < SN; ++i) o[nt][u][i] = (f32x4){(float)x[4 * i], (float)x[4 * i + 1], (float)x[4 * i + 2], (float)x[4 * i + 3]};
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < SN; ++i) o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + from + 4 * i);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < SN; ++i) o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + slot * D + dim0 + i * 16);
                     }
                 }
 #pragma unroll
@@ -991,6 +1007,9 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
             return packed_row(p, row0, kvh, row_lo + r);
         };
         __syncthreads();   // (the previous row block's results have left LDS)
+        const bool used = tid < 2 * pairs && tid < at.pages - 2 * at.first;   // pages from the first one of these steps on
+        int entry = -1;
+        if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + 2 * at.first + tid];
         const int last_pages = at.pages - 2 * (at.first + pairs - 1);   // of the last pair: 1 or 2 (or more follow)
         bf16x8 q[KS];
         {
@@ -999,10 +1018,6 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
             for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(row + 16 * ks + 8 * half);
         }
         {
-            const int have = at.pages - 2 * at.first;               // pages from the first one of these steps on
-            const bool used = tid < 2 * pairs && tid < have;
-            int entry = -1;
-            if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + 2 * at.first + tid];
             const bool bad = used && (unsigned)entry >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
             sh.page[tid] = bad ? -1 : entry;
             if (tid < 8) sh.page[2 * kMaxPrefixPairs + tid] = -1;
@@ -1232,7 +1247,7 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
                 for (int i = 0; i < 4; ++i) {
                     const f32x16 &x = acc[d2 * (SL / 2) + sl];
                     const f32x4 four = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                    unsigned char *at4 = o + c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * half) * kPartial;
+                    unsigned char *at4 = o + c32 * Sh::kOutRow + partial_place<D>(32 * sl + 8 * i + 4 * half) * kPartial;
                     if constexpr (FULL) *reinterpret_cast<f32x4 *>(at4) = four;
                     else *reinterpret_cast<f16x4 *>(at4) = __builtin_convertvector(four, f16x4);
                 }
