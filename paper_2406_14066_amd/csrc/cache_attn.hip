@@ -796,6 +796,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         rh[nt] = packed_row(p, w.row0, w.kvh, w.row_lo + min(r, rows - 1));
     }
     const int dim0 = wave * (SN * 16) + 4 * g;
+    // Partial results are read in rounds, whose loads are all on their way together: as many as the walk's registers hold, or a few
+    // where a few are left.
+    constexpr int kFew = NT <= 2 ? 4 : 2, kMany = (NT * D >= 256 ? 160 : 80) / (NT * (4 * SN + 2));
     if (prefix) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -836,11 +839,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         __syncthreads();
         if (!sh.last) return;
         order_after_ticket();
-        // the last chunk to finish: all of them in chunk order, a few of all rows on their way together
-        constexpr int U = NT <= 2 ? 4 : 2;
+        // the last chunk to finish: all of them in chunk order
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sum[nt].clear();
-        for (int c0 = 0; c0 < w.nchunks; c0 += U) {
+        auto add_chunks = [&](auto count, int c0) {
+            constexpr int U = decltype(count)::value;
             u32x2 ml[NT][U];
             u32x4 o[NT][U][SN];
 #pragma unroll
@@ -861,6 +864,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                     for (int i = 0; i < SN; ++i) x[i] = __builtin_bit_cast(f32x4, o[nt][u][i]);
                     if (c0 + u < w.nchunks) sum[nt].add(__uint_as_float(ml[nt][u].x), __uint_as_float(ml[nt][u].y), x);
                 }
+        };
+        for (int c0 = 0; c0 < w.nchunks;) {
+            if (w.nchunks - c0 > kFew) {
+                add_chunks(std::integral_constant<int, kMany>(), c0);
+                c0 += kMany;
+            } else {
+                add_chunks(std::integral_constant<int, kFew>(), c0);
+                c0 += kFew;
+            }
         }
     }
     // the prefix's partial results
@@ -868,40 +880,60 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) pieces[nt] = partials_of(min(nt * 16 + n16, rows - 1));
     if (w.prefix > 0) {
-        constexpr int U = NT <= 2 ? 4 : 2;
         int most = 0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) most = max(most, pieces[nt]);
-        for (int c0 = 0; __builtin_amdgcn_ballot_w64(c0 < most) != 0; c0 += U) {
+        auto add_pieces = [&](auto count, int c0) {
+            constexpr int U = decltype(count)::value;
             f32x2 ml[NT][U];
-            f32x4 o[NT][U][SN];
+            u32x4 o[NT][U][SN];   // as they were stored
+            constexpr int kHalves = SN == 2 ? 1 : 0;   // (fp16: a lane's two slices are 16 bytes)
+            const bool halves = !FULL && w.prefix_pairs > 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, pieces[nt] - 1);
                     ml[nt][u] = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
-                    if (w.prefix_pairs > 0) {   // (see partial_place)
-                        const size_t from = slot * D + wave * (SN * 16) + g * (SN * 4);
-                        if constexpr (!FULL) {
-                            typedef _Float16 Halves __attribute__((ext_vector_type(4 * SN)));
-                            const Halves x = *reinterpret_cast<const Halves *>(reinterpret_cast<const _Float16 *>(p.prefix_acc) + from);
-#pragma unroll
-                            for (int i = 0; i < SN; ++i) o[nt][u][i] = (f32x4){(float)x[4 * i], (float)x[4 * i + 1], (float)x[4 * i + 2], (float)x[4 * i + 3]};
+                    if (halves) {
+                        const _Float16 *from = reinterpret_cast<const _Float16 *>(p.prefix_acc) + slot * D + partial_place<D>(dim0);
+                        if constexpr (kHalves) {
+                            o[nt][u][0] = *reinterpret_cast<const u32x4 *>(from);
                         } else {
-#pragma unroll
-                            for (int i = 0; i < SN; ++i) o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + from + 4 * i);
+                            const u32x2 x = *reinterpret_cast<const u32x2 *>(from);
+                            o[nt][u][0] = (u32x4){x.x, x.y, 0u, 0u};
                         }
                     } else {
+                        const float *from = p.prefix_acc + slot * D;
 #pragma unroll
-                        for (int i = 0; i < SN; ++i) o[nt][u][i] = *reinterpret_cast<const f32x4 *>(p.prefix_acc + slot * D + dim0 + i * 16);
+                        for (int i = 0; i < SN; ++i)
+                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (w.prefix_pairs > 0 ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
                     }
                 }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (c0 + u < pieces[nt]) sum[nt].add(ml[nt][u].x, ml[nt][u].y, o[nt][u]);
+                for (int u = 0; u < U; ++u) {
+                    f32x4 x[SN];
+                    if (halves) {
+#pragma unroll
+                        for (int i = 0; i < SN; ++i)
+                            x[i] = __builtin_convertvector(__builtin_bit_cast(f16x4, (u32x2){o[nt][u][0][2 * i], o[nt][u][0][2 * i + 1]}), f32x4);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < SN; ++i) x[i] = __builtin_bit_cast(f32x4, o[nt][u][i]);
+                    }
+                    if (c0 + u < pieces[nt]) sum[nt].add(ml[nt][u].x, ml[nt][u].y, x);
+                }
+        };
+        for (int c0 = 0; __builtin_amdgcn_ballot_w64(c0 < most) != 0;) {
+            if (__builtin_amdgcn_ballot_w64(c0 + kFew < most) != 0) {
+                add_pieces(std::integral_constant<int, kMany>(), c0);
+                c0 += kMany;
+            } else {
+                add_pieces(std::integral_constant<int, kFew>(), c0);
+                c0 += kFew;
+            }
         }
     }
 #pragma unroll
