@@ -147,6 +147,8 @@ spec_status check_attn(const spec_prefix_attn_args *a)
     return SPEC_OK;
 }
 
+constexpr int kMostTiles = 3;   // row tiles of a block
+
 struct Plan {
     int row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
     int prefix_tiles, prefix_many_rows, prefix_block_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
@@ -154,30 +156,48 @@ struct Plan {
     int64_t blocks, prefix_blocks;
 };
 
-// Chunk length of jobs that a block streams through, from a model of the launch.  A block takes kBlockUs besides its tokens,
-// kSplitUs more where its job is split (partial results, a ticket, the merge); a token takes kTokenUs while a compute unit has
-// nothing else to do, and its bytes' share of the memory's rate where all units are busy, two blocks each.  The launch
-// ends with its longest block, or when the blocks have gone through their slots.
-constexpr double kBlockUs = 5.5, kSplitUs = 6.0, kTokenUs = 0.0065, kUnitBytesPerUs = 23000.0;
+// Row tiles of a block and chunk length for jobs of some tokens and query rows, from a model of the launch, fitted to single
+// requests and batches of 4 and 16 with 300 .. 16000 tokens (40 rows, d = 128) at every number of tiles and chunks.
+//
+// With n row tiles a block takes kBlockUs[n] and kTokenUs[n] for a token: more rows are more to multiply and to merge, and all wait
+// for the slowest wavefront (700 tokens of one request, 8-bit, n = 1, 2, 3: 8.3 / 10.0 / 12.2 us), but fewer tiles mean more blocks
+// that read the same pages.  A job of c chunks waits for its partial results and a ticket, and its last block reads c times its rows
+// (6000 tokens of one request, n = 1, c = 3, 6, 12, 24, 48: 19.0 / 15.6 / 18.0 / 36.6 / 56.7 us).  A second block on a compute
+// unit shares its issue slots and its share of the memory with the first, and adds a tenth to the rate; blocks beyond the first on each
+// unit end at different times, which costs half of the longest one.
+struct Split {
+    int tiles, length;
+};
+constexpr double kBlockUs[4] = {0.0, 4.7, 5.5, 6.7}, kTokenUs[4] = {0.0, 0.0052, 0.0064, 0.0078};
+constexpr double kFullFactor = 1.4;                                                  // of a token, with weights in more than one term
+constexpr double kTicketUs = 2.5, kJoinUs[4] = {0.0, 0.55, 0.75, 0.95};              // of a split job; of each of its chunks
+constexpr double kSecondBlock = 1.1;
 template <typename F>
-int chunk_length(int most_tokens, double token_bytes, F for_each_job)   // for_each_job(f): f(tokens, blocks per chunk)
+Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double ticket_us, F for_each_job)   // for_each_job(f): f(tokens, rows)
 {
     const int most = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
-    const double slots = 2.0 * compute_units(), token_us = 2.0 * token_bytes / kUnitBytesPerUs;
-    int best = most;
+    const double units = compute_units();
+    const int most_tiles = std::min((most_rows + 15) / 16, kMostTiles);
+    Split best = {most_tiles, most};
     double best_us = 1e30;
-    for (int len = most; len >= kPairTokens; len = len * 3 / 4 / kPairTokens * kPairTokens) {
-        double longest = 0.0, sum = 0.0;
-        for_each_job([&](int tokens, int64_t blocks) {
-            const int chunks = std::max((tokens + len - 1) / len, 1), each = (tokens + chunks - 1) / chunks;
-            const double fixed = kBlockUs + (chunks > 1 ? kSplitUs : 0.0);
-            longest = std::max(longest, fixed + each * kTokenUs);
-            sum += (double)blocks * chunks * (fixed + each * token_us);
-        });
-        const double us = std::max(longest, sum / slots);
-        if (us < best_us * 0.97) {   // (shorter chunks only for something)
-            best_us = us;
-            best = len;
+    for (int tiles = most_tiles; tiles >= 1; --tiles) {
+        const double token_us = kTokenUs[tiles] * (full ? kFullFactor : 1.0);
+        for (int len = most; len >= kPairTokens; len = len * 3 / 4 / kPairTokens * kPairTokens) {
+            double longest = 0.0, sum = 0.0, count = 0.0;
+            for_each_job([&](int tokens, int64_t rows) {
+                const int chunks = std::max((tokens + len - 1) / len, 1), each = (tokens + chunks - 1) / chunks;
+                const double blocks = (double)((rows + 16 * tiles - 1) / (16 * tiles)) * Hkv * chunks;
+                const double us = kBlockUs[tiles] + each * token_us, join_us = chunks > 1 ? ticket_us + chunks * kJoinUs[tiles] : 0.0;
+                longest = std::max(longest, us + join_us);
+                sum += blocks * us;
+                count += blocks;
+            });
+            const double busy = sum / (units * kSecondBlock), us = std::max(longest, count > units ? busy + 0.5 * longest : 0.0);
+            if (us < best_us * 0.97) {   // (fewer tiles or shorter chunks only for something)
+                best_us = us;
+                best = {tiles, len};
+            }
+            if (busy >= best_us) break;   // (shorter chunks are more work in all)
         }
     }
     return best;
@@ -200,8 +220,8 @@ Plan make_plan(const spec_prefix_attn_args *a)
 {
     Plan pl;
     memset(&pl, 0, sizeof pl);
-    const int group = a->Hq / a->Hkv, most_tiles = 3;
-    const double token_bytes = a->kv_dtype == SPEC_BF16 ? 4.0 * a->d : 2.0 * a->d + 8.0;   // of a KV head
+    const int group = a->Hq / a->Hkv;
+    const bool full = a->out_dtype == SPEC_F32;
     int max_q = 0, max_own = 0, max_len = 0;
     auto prefix_of = [&](int &g, int b) {
         if (a->G == 0) return 0;
@@ -219,15 +239,15 @@ Plan make_plan(const spec_prefix_attn_args *a)
     const int max_rows = std::max(max_q * group, 1);
     pl.max_q_rows = max_rows;
     pl.capacity = a->max_kv_len > 0 ? a->max_kv_len : max_len;
-    pl.row_tiles = std::min((max_rows + 15) / 16, most_tiles);
-    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
-    pl.chunk_tokens = chunk_length(max_own, token_bytes, [&](auto job) {
+    const Split own = split_jobs(max_rows, max_own, a->Hkv, full, kTicketUs, [&](auto job) {
         for (int b = 0, g = 0; b < a->B; ++b) {
             const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = prefix_of(g, b);
-            if (q == 0) continue;
-            job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, (int64_t)((q * group + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles)) * a->Hkv);
+            if (q > 0) job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, q * group);
         }
     });
+    pl.row_tiles = own.tiles;
+    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
+    pl.chunk_tokens = own.length;
     pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
     pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
     int max_prefix = 0;
@@ -238,7 +258,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
     }
     if (max_prefix > 0 && most_rows > 0) {
         pl.prefix_capacity = max_prefix;
-        pl.prefix_many_rows = most_rows > 16 * most_tiles;
+        pl.prefix_many_rows = most_rows > 16 * kMostTiles;
         auto rows_of = [&](int g) { return (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group; };
         if (pl.prefix_many_rows) {
             auto pairs_of = [&](int g) { return (a->host_prefix_len[g] + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE); };
@@ -251,14 +271,14 @@ Plan make_plan(const spec_prefix_attn_args *a)
             // partial results of a row block: one of each block that its steps touch
             pl.max_prefix_chunks = ((max_prefix + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE) + pl.prefix_block_steps - 2) / pl.prefix_block_steps + 1;
         } else {
-            pl.prefix_tiles = (int)std::min<int64_t>((most_rows + 15) / 16, most_tiles);
-            auto row_blocks_of = [&](int g) { return (rows_of(g) + 16 * pl.prefix_tiles - 1) / (16 * pl.prefix_tiles); };
-            // (as many as the rows can make however they are spread over the groups)
-            pl.prefix_row_blocks = (int)((int64_t)a->T * group / (16 * pl.prefix_tiles)) + a->G;
-            pl.prefix_chunk_tokens = chunk_length(max_prefix, token_bytes, [&](auto job) {
+            const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, full, 0.0, [&](auto job) {   // (no ticket: the next launch joins)
                 for (int g = 0; g < a->G; ++g)
-                    if (a->host_prefix_len[g] > 0) job(a->host_prefix_len[g], row_blocks_of(g) * a->Hkv);
+                    if (a->host_prefix_len[g] > 0) job(a->host_prefix_len[g], rows_of(g));
             });
+            pl.prefix_tiles = split.tiles;
+            pl.prefix_chunk_tokens = split.length;
+            // (as many row blocks as the rows can make however they are spread over the groups)
+            pl.prefix_row_blocks = (int)((int64_t)a->T * group / (16 * pl.prefix_tiles)) + a->G;
             pl.max_prefix_chunks = (max_prefix + pl.prefix_chunk_tokens - 1) / pl.prefix_chunk_tokens;
             pl.prefix_blocks = (int64_t)pl.prefix_row_blocks * a->Hkv * pl.max_prefix_chunks;
         }
