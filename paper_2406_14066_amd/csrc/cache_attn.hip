@@ -438,13 +438,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     const int npages = (w.tok1 - w.tok0 + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE;   // <= 64 * kWaves
     const int mine = 2 * (wave + kWaves * (lane >> 1)) + (lane & 1);
     int bt = -1;
+    bool some_bad;
     {
         const bool used = mine < npages;
         if (used) bt = p.block_table[(size_t)w.b * p.max_blocks_per_req + w.tok0 / SPEC_BLOCK_SIZE + mine];
         const bool bad = used && (unsigned)bt >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
         if (bad) bt = -1;
         const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
-        if (bad_lanes != 0 && w.kvh == 0 && w.row_block == 0 && lane == 0 && p.errors != nullptr)
+        some_bad = bad_lanes != 0;
+        if (some_bad && w.kvh == 0 && w.row_block == 0 && lane == 0 && p.errors != nullptr)
             atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
     }
     const int npairs = (npages + 1) / 2;
@@ -465,30 +467,29 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     // for which the hardware returns zeros without touching memory.
     const char *khead = static_cast<const char *>(p.k_cache) + (size_t)w.kvh * kPageBytes;
     const char *vhead = static_cast<const char *>(p.v_cache) + (size_t)w.kvh * kPageBytes;
-    const size_t page_stride = (size_t)p.Hkv * kPageBytes;
+    const uint32_t page_stride = (uint32_t)p.Hkv * kPageBytes;
     Pair<KIND, D> cur;
-    auto page_of = [&](int i, int h, bool &valid) {
-        const int entry = __builtin_amdgcn_readlane(bt, i < my_pairs ? 2 * i + h : 0);
-        valid = i < my_pairs && entry >= 0;
-        return (size_t)(valid ? entry : 0);
+    auto page_of = [&](int i, int h) {   // -1: none.  (past the last pair that a wavefront can have: that one again, and not used)
+        return __builtin_amdgcn_readlane(bt, 2 * min(i, kWave / 2 - 1) + h);
+    };
+    auto page_descriptor = [&](const char *head, int page) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(head + (uint64_t)(uint32_t)page * page_stride), 0, page < 0 ? 0 : kPageBytes, kBufferFlags);
     };
     auto load_k = [&](int i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bool valid;
-            const size_t page = page_of(i, h, valid);
-            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + page * page_stride), 0, valid ? kPageBytes : 0, kBufferFlags);
+            const __amdgpu_buffer_rsrc_t kd = page_descriptor(khead, page_of(i, h));
 #pragma unroll
             for (int j = 0; j < Pair<KIND, D>::N; ++j)
                 cur.k[h][j] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, j * 64, 0)
                                  : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, j * 1024, kStreamPolicy);
         }
     };
+    const char *scales_at = reinterpret_cast<const char *>(p.kv_scale + w.kvh * 32 + 4 * g + (n16 & 3));
     auto load_scales = [&](int i) {
         if constexpr (B8) {   // (no branch: a page that is not there is read as page 0, and not used)
-            bool valid;
-            const size_t page0 = page_of(i, 0, valid), page1 = page_of(i, 1, valid);
-            const float *at = p.kv_scale + (((n16 & 4) ? page1 : page0) * p.Hkv + w.kvh) * 32 + 4 * g + (n16 & 3);
+            const uint32_t page0 = max(page_of(i, 0), 0), page1 = max(page_of(i, 1), 0);
+            const float *at = reinterpret_cast<const float *>(scales_at + (uint64_t)((n16 & 4) ? page1 : page0) * (uint32_t)(p.Hkv * 128));
             cur.ks = at[0];
             cur.vs = at[16];
         }
@@ -496,9 +497,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     auto load_v = [&](int i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bool valid;
-            const size_t page = page_of(i, h, valid);
-            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + page * page_stride), 0, valid ? kPageBytes : 0, kBufferFlags);
+            const __amdgpu_buffer_rsrc_t vd = page_descriptor(vhead, page_of(i, h));
 #pragma unroll
             for (int j = 0; j < Pair<KIND, D>::N; ++j) cur.v[h][j] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, j * 1024, kStreamPolicy);
         }
@@ -534,11 +533,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     }
 
     // Each part of a pair's registers takes the next pair as soon as it has been used.
-    // (masked: some of the pair's tokens are hidden from some row, or past the end)
+    // (masked: some of the pair's tokens are hidden from some row, or past the end, or some page is not there)
     auto step = [&](int i, auto masked) {
         constexpr bool need_mask = decltype(masked)::value;
         const int first = w.tok0 + 2 * (wave + kWaves * i) * SPEC_BLOCK_SIZE;
-        asm volatile("" : "+v"(q_at));   // (the query rows are read from LDS in every step, not kept in registers)
+        if constexpr (NT > 1) asm volatile("" : "+v"(q_at));   // (the query rows are read from LDS in every step, not kept in registers)
         // scores
         f32x4 s[NT][2];
 #pragma unroll
@@ -564,11 +563,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         // the row and handed to the others)
         f32x4 ks[2], lv[2], rv[2];
         if constexpr (B8) {
-            bool there[2];
-            (void)page_of(i, 0, there[0]);
-            (void)page_of(i, 1, there[1]);
-            const bool on = (n16 & 4) ? there[1] : there[0];   // (a page that reads as zeros)
-            const float k1 = on ? cur.ks * p.scale_log2 : 0.0f, v1 = !on || cur.vs < kSmallestScale ? kSmallestScale : cur.vs;
+            float k1 = cur.ks * p.scale_log2, v1 = __builtin_elementwise_maximum(cur.vs, kSmallestScale);
+            if (need_mask) {
+                const bool on = ((n16 & 4) ? page_of(i, 1) : page_of(i, 0)) >= 0;   // (a page that reads as zeros)
+                k1 = on ? k1 : 0.0f;
+                v1 = on ? v1 : kSmallestScale;
+            }
             const float l1 = __builtin_amdgcn_logf(v1), r1 = __builtin_amdgcn_rcpf(v1);
             auto hand_out = [&](float x, f32x4(&to)[2]) {
                 to[0] = (f32x4){row_broadcast<0>(x), row_broadcast<1>(x), row_broadcast<2>(x), row_broadcast<3>(x)};
@@ -586,12 +586,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[nt][h][r] = B8 ? fmaf(s[nt][h][r], ks[h][r], lv[h][r]) : s[nt][h][r] * p.scale_log2;
+                    if constexpr (B8) s[nt][h][r] = fmaf(s[nt][h][r], ks[h][r], lv[h][r]);
                     if (need_mask && first + h * SPEC_BLOCK_SIZE + 4 * g + r > min(limit[nt], w.tok1 - 1)) s[nt][h][r] = -INFINITY;
                 }
             }
             float mx = max3(max3(s[nt][0][0], s[nt][0][1], s[nt][0][2]), max3(s[nt][0][3], s[nt][1][0], s[nt][1][1]), __builtin_elementwise_maximum(s[nt][1][2], s[nt][1][3]));
-            mx -= kTop;
+            mx = B8 ? mx - kTop : mx * p.scale_log2;   // (the scale is positive: the maximum commutes with it)
             const float most = m_run[nt] + kRescaleSlack;
             if (__builtin_amdgcn_ballot_w64(mx > most) != 0) {
                 mx = max_across_xor32(max_across_xor16(mx));
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = fast_exp2(s[nt][h][r] - m_run[nt]);
+                    const float e = fast_exp2(B8 ? s[nt][h][r] - m_run[nt] : fmaf(s[nt][h][r], p.scale_log2, -m_run[nt]));
                     float part = e;
                     if constexpr (B8) {
                         part = e * rv[h][r];
@@ -702,7 +702,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                     for (int t = 0; t < 2 * SPEC_BLOCK_SIZE; ++t) {
                         const int slot = t % SPEC_BLOCK_SIZE, entry = at[t / SPEC_BLOCK_SIZE];
                         if (first + t >= w.tok1 || entry < 0) continue;
-                        const uint16_t *page = reinterpret_cast<const uint16_t *>(vhead + (size_t)entry * page_stride);
+                        const uint16_t *page = reinterpret_cast<const uint16_t *>(vhead + (uint64_t)entry * page_stride);
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     };
 
     const int all_see = min(w.tok1, w.hide_from) - w.tok0;   // tokens that every row sees
-    const int plain = min(my_pairs, all_see / (2 * SPEC_BLOCK_SIZE) > wave ? (all_see / (2 * SPEC_BLOCK_SIZE) - wave + kWaves - 1) / kWaves : 0);
+    const int plain = some_bad ? 0 : min(my_pairs, all_see / (2 * SPEC_BLOCK_SIZE) > wave ? (all_see / (2 * SPEC_BLOCK_SIZE) - wave + kWaves - 1) / kWaves : 0);
     int i = 0;
     for (; i < plain; ++i) step(i, std::false_type());
     for (; i < my_pairs; ++i) step(i, std::true_type());
