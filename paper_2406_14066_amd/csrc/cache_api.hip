@@ -211,8 +211,8 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double tick
 int prefix_block_steps(int64_t steps)
 {
     const int64_t units = compute_units();
-    const int64_t slots = steps >= 3 * units * 12 ? 3 * units : units;
-    const int64_t rounds = (steps + slots * kMaxPrefixPairs - 1) / (slots * kMaxPrefixPairs);
+    const int64_t slots = steps >= 2 * units * 6 ? 2 * units : units;
+    const int64_t rounds = (steps + slots * kMaxPrefixSteps - 1) / (slots * kMaxPrefixSteps);
     return (int)std::max<int64_t>((steps + slots * rounds - 1) / (slots * rounds), 1);
 }
 
@@ -261,15 +261,16 @@ Plan make_plan(const spec_prefix_attn_args *a)
         pl.prefix_many_rows = most_rows > 16 * kMostTiles;
         auto rows_of = [&](int g) { return (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group; };
         if (pl.prefix_many_rows) {
-            auto pairs_of = [&](int g) { return (a->host_prefix_len[g] + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE); };
+            constexpr int kStepTokens = kStepPages * SPEC_BLOCK_SIZE;
+            auto walk_of = [&](int tokens) { return (tokens + kStepTokens - 1) / kStepTokens; };
             int64_t steps = 0;
-            for (int g = 0; g < a->G; ++g) steps += (rows_of(g) + kPrefixRows - 1) / kPrefixRows * pairs_of(g);
+            for (int g = 0; g < a->G; ++g) steps += (rows_of(g) + kPrefixRows - 1) / kPrefixRows * walk_of(a->host_prefix_len[g]);
             steps *= a->Hkv;
             pl.prefix_block_steps = prefix_block_steps(steps);
             pl.prefix_blocks = ((steps + pl.prefix_block_steps - 1) / pl.prefix_block_steps + kXcdCount - 1) / kXcdCount * kXcdCount;
             pl.prefix_row_blocks = (int)pl.prefix_blocks;
             // partial results of a row block: one of each block that its steps touch
-            pl.max_prefix_chunks = ((max_prefix + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE) + pl.prefix_block_steps - 2) / pl.prefix_block_steps + 1;
+            pl.max_prefix_chunks = (walk_of(max_prefix) + pl.prefix_block_steps - 2) / pl.prefix_block_steps + 1;
         } else {
             const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, full, 0.0, [&](auto job) {   // (no ticket: the next launch joins)
                 for (int g = 0; g < a->G; ++g)

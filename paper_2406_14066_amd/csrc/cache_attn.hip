@@ -97,7 +97,7 @@ struct Work {
     int group_index, first_of_group, end_of_group;    // its group, and (lane-wise, groups 0 .. 63) every group's requests and prefix
     int prefix_of_group;
     int prefix_chunks;                // partial results that come in from the prefix launch
-    int prefix_base, prefix_pairs;    // ... with many rows: the group's first step on this KV head, the steps of a row block
+    int prefix_base, prefix_walk;    // ... with many rows: the group's first step on this KV head, the steps of a row block
     int prefix_row0;                  // ... and its first packed token row
     int row_block;
 };
@@ -145,22 +145,22 @@ __device__ __forceinline__ int chunk_count(int tokens, int chunk_tokens) { retur
 
 // Steps of the launch for prefixes with many query rows (see prefix_rows_kernel): of all groups of a KV head in `total`,
 // of the groups before group `upto` as the result.
-__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int b0, int b1, int P, int &pairs, int &rows, int &row0)
+__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int b0, int b1, int P, int &walk, int &rows, int &row0)
 {
-    pairs = rows = row0 = 0;
+    walk = rows = row0 = 0;
     if (b0 < 0 || b0 > b1 || b1 > p.B || !prefix_ok(p, P)) return 0;
     row0 = p.cu_q_len[b0];
     const int end = p.cu_q_len[b1];
     rows = (end - row0) * p.group;
     if (row0 < 0 || end > p.T || rows <= 0) return 0;
-    pairs = (P + 2 * SPEC_BLOCK_SIZE - 1) / (2 * SPEC_BLOCK_SIZE);
-    return (rows + kPrefixRows - 1) / kPrefixRows * pairs;
+    walk = (P + kStepPages * SPEC_BLOCK_SIZE - 1) / (kStepPages * SPEC_BLOCK_SIZE);
+    return (rows + kPrefixRows - 1) / kPrefixRows * walk;
 }
 
-__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int g, int &pairs, int &rows)
+__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int g, int &walk, int &rows)
 {
     int row0;
-    return group_steps(p, p.cu_group[g], p.cu_group[g + 1], p.prefix_len[g], pairs, rows, row0);
+    return group_steps(p, p.cu_group[g], p.cu_group[g + 1], p.prefix_len[g], walk, rows, row0);
 }
 
 __device__ __forceinline__ int prefix_steps(const CacheAttnParams &p, int upto, int &total)
@@ -168,7 +168,7 @@ __device__ __forceinline__ int prefix_steps(const CacheAttnParams &p, int upto, 
     const int lane = threadIdx.x % kWave;
     int all = 0, before = 0;
     for (int base = 0; base < p.G; base += kWave) {
-        int pairs, rows, n = base + lane < p.G ? group_steps(p, base + lane, pairs, rows) : 0;
+        int walk, rows, n = base + lane < p.G ? group_steps(p, base + lane, walk, rows) : 0;
         int some = base + lane < upto ? n : 0;
 #pragma unroll
         for (int off = kWave / 2; off > 0; off >>= 1) {
@@ -184,22 +184,22 @@ __device__ __forceinline__ int prefix_steps(const CacheAttnParams &p, int upto, 
 
 struct PrefixPlace {
     int request, row0, rows;    // the group's first request, its first packed token row, its fused query rows
-    int row_block, first;       // row block of the step, and the step's pair of pages
-    int pairs, pages;           // of the prefix
+    int row_block, first;       // row block of the step, and which of its steps it is
+    int walk, pages;            // steps of a row block, pages of the prefix
 };
 
 // The groups base .. base + 63, a lane each.
 struct GroupLanes {
-    int b0, pages, row0, rows, pairs;
+    int b0, pages, row0, rows, walk;
     int steps, upto;   // of the group; of it and the lanes before it
     __device__ __forceinline__ void look(const CacheAttnParams &p, int base)
     {
         const int lane = threadIdx.x % kWave, g = base + lane;
-        steps = b0 = pages = row0 = rows = pairs = 0;
+        steps = b0 = pages = row0 = rows = walk = 0;
         if (g < p.G) {
             b0 = p.cu_group[g];
             const int b1 = p.cu_group[g + 1], P = p.prefix_len[g];
-            steps = group_steps(p, b0, b1, P, pairs, rows, row0);
+            steps = group_steps(p, b0, b1, P, walk, rows, row0);
             pages = P / SPEC_BLOCK_SIZE;
         }
         upto = steps;
@@ -217,13 +217,13 @@ struct GroupLanes {
         if (holds == 0) return false;
         const int who = __builtin_ctzll(holds);
         const int rest = step - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(steps, who));
-        at.pairs = __builtin_amdgcn_readlane(pairs, who);
+        at.walk = __builtin_amdgcn_readlane(walk, who);
         at.rows = __builtin_amdgcn_readlane(rows, who);
         at.row0 = __builtin_amdgcn_readlane(row0, who);
         at.request = __builtin_amdgcn_readlane(b0, who);
         at.pages = __builtin_amdgcn_readlane(pages, who);
-        at.row_block = rest / at.pairs;
-        at.first = rest - at.row_block * at.pairs;
+        at.row_block = rest / at.walk;
+        at.first = rest - at.row_block * at.walk;
         return true;
     }
 };
@@ -290,7 +290,7 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
 __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w)
 {
     w.prefix_chunks = 0;
-    w.prefix_pairs = 0;
+    w.prefix_walk = 0;
     if (w.prefix == 0) return true;
     if (!p.prefix_many_rows) {
         w.prefix_chunks = chunk_count(w.prefix, p.prefix_chunk_tokens);
@@ -299,10 +299,10 @@ __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w
     int total, before, rows;
     if (p.G <= kWave) {
         const int lane = threadIdx.x % kWave;
-        int pairs = 0, all_rows = 0, row0 = 0;
-        int n = lane < p.G ? group_steps(p, w.first_of_group, w.end_of_group, w.prefix_of_group, pairs, all_rows, row0) : 0;
+        int walk = 0, all_rows = 0, row0 = 0;
+        int n = lane < p.G ? group_steps(p, w.first_of_group, w.end_of_group, w.prefix_of_group, walk, all_rows, row0) : 0;
         int some = lane < w.group_index ? n : 0;
-        w.prefix_pairs = __builtin_amdgcn_readlane(n, w.group_index) > 0 ? __builtin_amdgcn_readlane(pairs, w.group_index) : 0;
+        w.prefix_walk = __builtin_amdgcn_readlane(n, w.group_index) > 0 ? __builtin_amdgcn_readlane(walk, w.group_index) : 0;
         rows = __builtin_amdgcn_readlane(all_rows, w.group_index);
         w.prefix_row0 = __builtin_amdgcn_readlane(row0, w.group_index);
 #pragma unroll
@@ -314,11 +314,11 @@ __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w
         before = __builtin_amdgcn_readfirstlane(some);
     } else {
         before = prefix_steps(p, w.group_index, total);
-        if (group_steps(p, w.group_index, w.prefix_pairs, rows) == 0) w.prefix_pairs = 0;
-        w.prefix_row0 = w.prefix_pairs > 0 ? uniform_load(p.cu_q_len, uniform_load(p.cu_group, w.group_index)) : 0;
+        if (group_steps(p, w.group_index, w.prefix_walk, rows) == 0) w.prefix_walk = 0;
+        w.prefix_row0 = w.prefix_walk > 0 ? uniform_load(p.cu_q_len, uniform_load(p.cu_group, w.group_index)) : 0;
     }
     const int after = (w.row0 - w.prefix_row0) * p.group;   // the request's rows lie in its group's
-    if ((int64_t)total * p.Hkv > (int64_t)p.prefix_row_blocks * p.prefix_block_steps || w.prefix_pairs == 0 || after < 0 ||
+    if ((int64_t)total * p.Hkv > (int64_t)p.prefix_row_blocks * p.prefix_block_steps || w.prefix_walk == 0 || after < 0 ||
         after + w.rows > rows) {
         count_error(p, w.chunk == 0 && w.kvh == 0 && w.row_block == 0);
         return false;
@@ -509,10 +509,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     // Partial results of the block's row r: those of the blocks from the one that took the first step of its row block to the one that
     // took the last (many rows), or one of each chunk.
     auto partials_of = [&](int r) {
-        if (w.prefix_pairs == 0) return w.prefix_chunks;
+        if (w.prefix_walk == 0) return w.prefix_chunks;
         const int rr = (w.row0 - w.prefix_row0) * p.group + w.row_lo + r;
-        const int step = w.prefix_base + rr / kPrefixRows * w.prefix_pairs;
-        return (step + w.prefix_pairs - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
+        const int step = w.prefix_base + rr / kPrefixRows * w.prefix_walk;
+        return (step + w.prefix_walk - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
     };
 #pragma unroll
     for (int k = 0; k < QN; ++k) {
@@ -888,7 +888,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
             f32x2 ml[NT][U];
             u32x4 o[NT][U][SN];   // as they were stored
             constexpr int kHalves = SN == 2 ? 1 : 0;   // (fp16: a lane's two slices are 16 bytes)
-            const bool halves = !FULL && w.prefix_pairs > 0;
+            const bool halves = !FULL && w.prefix_walk > 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -907,7 +907,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                         const float *from = p.prefix_acc + slot * D;
 #pragma unroll
                         for (int i = 0; i < SN; ++i)
-                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (w.prefix_pairs > 0 ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
+                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (w.prefix_walk > 0 ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
                     }
                 }
 #pragma unroll
@@ -955,48 +955,47 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 // ---------------------------------------------------------------------------
 // Prefixes of groups with many query rows.
 //
-// The work is counted in (row block of 128 rows, pair of pages) steps, laid out KV head by KV head, group by group, row block
+// The work is counted in (row block of 128 rows, four pages) steps, laid out KV head by KV head, group by group, row block
 // by row block; every block takes the same number of consecutive steps, whatever row blocks they belong to, and leaves a
 // partial result for each row block it touches.  So all blocks end together however ragged the groups are, and the blocks
 // of an XCD share their KV heads' pages in its L2.
 //
-// A block's four wavefronts have 32 rows each and walk the same pages, which pass through LDS once for all of them, a pair
-// of pages (32 tokens) at a time.  In LDS a pair lies as the operands of v_mfma_f32_32x32x16 want it, 16 bytes per lane
-// and 1 KB per read, as 16-bit values whatever the cache holds (8-bit codes are converted once on the way in);
-// token-major V is stored by rows and read through the transposing read.  (lane = 32 half + c)
-//   S^T[token][row] = K[token][:] . Q[row][:]: 16 dims per instruction, lane (half, c) holds row c, tokens
+// A block's four wavefronts have 32 rows each and walk the same pages, which pass through LDS once for all of them, a step
+// (64 tokens, a page brought in by each wavefront) at a time.  In LDS the pages lie as the operands of v_mfma_f32_32x32x16 want
+// them, 16 bytes per lane and 1 KB per read, as 16-bit values whatever the cache holds (8-bit codes are converted once on the
+// way in); token-major V is stored by rows and read through the transposing read.  (lane = 32 half + c; pair: two of the pages)
+//   S^T[token][row] = K[token][:] . Q[row][:]: a pair, 16 dims per instruction, lane (half, c) holds row c, tokens
 //   4 half + 8 i + 0..3, i = 0, 1 of the first page, 2, 3 of the second
 //   O^T[dim][row] += V^T[dim][token] . P^T[token][row]: a page per instruction, its tokens in that order
-// Two LDS buffers and one barrier per pair.  Blocks of a compute unit are not in step with each other, and that is what
-// keeps its matrix cores and its vector units busy at the same time.
+// Two LDS buffers and one barrier per step.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int KIND, int D>
 struct RowsShared {
-    static constexpr int kK = 2 * SPEC_BLOCK_SIZE * D * 2;   // of a pair
-    static constexpr int kV = 2 * SPEC_BLOCK_SIZE * (KIND == kCacheTokens ? v_row_bytes(D) : D * 2);
+    static constexpr int kK = kStepPages * SPEC_BLOCK_SIZE * D * 2;   // of a step
+    static constexpr int kV = kStepPages * SPEC_BLOCK_SIZE * (KIND == kCacheTokens ? v_row_bytes(D) : D * 2);
     static constexpr int kOutRow = D * 2 + 16;               // half a result row
     union {
         struct {
-            alignas(16) unsigned char k[2][kK];   // [16-dim step][lane][16]
+            alignas(16) unsigned char k[2][kK];   // [pair][16 dims][lane][16]
             alignas(16) unsigned char v[2][kV];   // [page][32-dim slice][lane][tokens 4 half .. + 3, 8 + 4 half .. + 3]; token-major: [page][token] rows
         };
         alignas(16) unsigned char o[kWaves][32 * kOutRow];   // results on their way out, by half rows
     };
     // 8-bit pages, per token: K's scale with the softmax scale, log2 of V's, its reciprocal
-    float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? 2 * SPEC_BLOCK_SIZE : 1];
-    int page[2 * kMaxPrefixPairs + 8];   // (one for each thread, and four more pairs)
-    static_assert(2 * kMaxPrefixPairs == kThreads, "a thread per page");   // the steps' block-table entries; -1: outside the pool, or past the end
+    float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? kStepPages * SPEC_BLOCK_SIZE : 1];
+    int page[kStepPages * (kMaxPrefixSteps + 4)];   // the steps' block-table entries, and four more steps'; -1: outside the pool, or past the end
+    static_assert(kStepPages * kMaxPrefixSteps == kThreads, "a thread per page");
+    GroupLanes groups[kWave];
 };
 
 template <int KIND, int D, bool FULL>
-__global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParams p)
+__global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParams p)
 {
     constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;
     constexpr int KS = D / 16, SL = D / 32;
     constexpr int kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);
     constexpr int N = B8 ? D / 64 : D / 32;              // 1 KB pieces of a page's K, of its V
-    constexpr int PN = N >= 2 ? N / 2 : 1;               // ... that a wavefront brings in
     constexpr int TERMS = FULL ? (B8 ? 2 : 3) : 1;
     constexpr float kTop = B8 ? 7.0f : 0.0f;
     typedef std::conditional_t<B8, f16x8, bf16x8> Weights;
@@ -1008,29 +1007,33 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
     // consecutive blocks go to different XCDs; consecutive steps stay on one
     const int block = (int)(blockIdx.x % kXcdCount) * (gridDim.x / kXcdCount) + blockIdx.x / kXcdCount;
 
-    GroupLanes groups;
-    groups.look(p, 0);
-    int total = groups.total();   // steps of a KV head
+    // the first 64 groups, kept in LDS (the walk needs the registers)
+    int total;   // steps of a KV head
+    {
+        GroupLanes groups;
+        groups.look(p, 0);
+        total = groups.total();
+        if (wave == 0) sh.groups[lane] = groups;
+    }
     if (p.G > kWave) prefix_steps(p, -1, total);
     if ((int64_t)total * p.Hkv > (int64_t)gridDim.x * p.prefix_block_steps) return;   // (not the groups planned for: the own launch reports it)
     int pos = block * p.prefix_block_steps;
     const int end = min(pos + p.prefix_block_steps, total * p.Hkv);
+    __syncthreads();   // the groups are in LDS
 
     while (pos < end) {
         // the row block that step `pos` belongs to
         const int kvh = pos / total;
         PrefixPlace at = {};
         int step = pos - kvh * total;
-        if (p.G <= kWave) {
-            groups.find(step, at);
-        } else {
-            for (int base = 0; base < p.G; base += kWave) {
-                groups.look(p, base);
-                if (groups.find(step, at)) break;
-                step -= groups.total();
-            }
+        for (int base = 0; base < p.G; base += kWave) {
+            GroupLanes groups;
+            if (base == 0) groups = sh.groups[lane];
+            else groups.look(p, base);
+            if (groups.find(step, at)) break;
+            step -= groups.total();
         }
-        const int pairs = min(at.pairs - at.first, end - pos);
+        const int steps = min(at.walk - at.first, end - pos);
         const int slot = block - (pos - at.first) / p.prefix_block_steps;
         const int row0 = at.row0;                                   // the group's first packed token row
         const int row_lo = at.row_block * kPrefixRows + wave * 32;
@@ -1039,10 +1042,10 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
             return packed_row(p, row0, kvh, row_lo + r);
         };
         __syncthreads();   // (the previous row block's results have left LDS)
-        const bool used = tid < 2 * pairs && tid < at.pages - 2 * at.first;   // pages from the first one of these steps on
+        const bool used = tid < kStepPages * steps && tid < at.pages - kStepPages * at.first;   // pages from the first one of these steps on
         int entry = -1;
-        if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + 2 * at.first + tid];
-        const int last_pages = at.pages - 2 * (at.first + pairs - 1);   // of the last pair: 1 or 2 (or more follow)
+        if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + kStepPages * at.first + tid];
+        const int last_pages = at.pages - kStepPages * (at.first + steps - 1);   // of the last step: 1 .. 4 (or more follow)
         bf16x8 q[KS];
         {
             const __bf16 *row = query_row(p, row0, kvh, c32 < rows ? row_lo + c32 : 0);
@@ -1052,79 +1055,75 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
         {
             const bool bad = used && (unsigned)entry >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
             sh.page[tid] = bad ? -1 : entry;
-            if (tid < 8) sh.page[2 * kMaxPrefixPairs + tid] = -1;
+            if (tid < 4 * kStepPages) sh.page[kThreads + tid] = -1;
             const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
             if (bad_lanes != 0 && kvh == 0 && at.row_block == 0 && lane == 0 && p.errors != nullptr)
                 atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
         }
         __syncthreads();
 
-        // Wavefront w brings in pieces w / 2, w / 2 + 2 of K and of V of page w % 2.
-        const int my_page = wave & 1, j0 = wave >> 1;
+        // Wavefront w brings in page w of a step.
         const char *khead = static_cast<const char *>(p.k_cache) + (size_t)kvh * kPageBytes;
         const char *vhead = static_cast<const char *>(p.v_cache) + (size_t)kvh * kPageBytes;
-        const size_t page_stride = (size_t)p.Hkv * kPageBytes;
+        const uint32_t page_stride = (uint32_t)p.Hkv * kPageBytes;
         struct {
-            u32x4 k[PN], v[PN];
-            float scale;   // 8-bit, wavefronts 0 and 1: the page's record, an entry per lane
+            u32x4 k[N], v[N];
+            float scale;   // 8-bit: the page's record, an entry per lane
         } in;
-        auto load = [&](int u) {
-            if (N == 1 && wave >= 2) return;   // (two pieces in all)
-            const int entry = __builtin_amdgcn_readfirstlane(sh.page[2 * u + my_page]);
-            const bool valid = entry >= 0;
-            const size_t page = (size_t)(valid ? entry : 0);
-            const int bytes = valid ? kPageBytes : 0;
-            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + page * page_stride), 0, bytes, kBufferFlags);
-            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + page * page_stride), 0, bytes, kBufferFlags);
+        auto load = [&](int page_entry) {
+            const int entry = __builtin_amdgcn_readfirstlane(page_entry);
+            const uint64_t at = (uint64_t)(uint32_t)entry * page_stride;
+            const int bytes = entry < 0 ? 0 : kPageBytes;
+            const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + at), 0, bytes, kBufferFlags);
+            const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + at), 0, bytes, kBufferFlags);
 #pragma unroll
-            for (int i = 0; i < PN; ++i) {
-                in.k[i] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, (j0 + 2 * i) * 64, 0)
-                             : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, (j0 + 2 * i) * 1024, 0);
-                in.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, (j0 + 2 * i) * 1024, 0);
+            for (int j = 0; j < N; ++j) {
+                in.k[j] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, j * 64, 0)
+                             : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, j * 1024, 0);
+                in.v[j] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, j * 1024, 0);
             }
             if constexpr (B8) {
                 const __amdgpu_buffer_rsrc_t sd = __builtin_amdgcn_make_buffer_rsrc(
-                    const_cast<float *>(p.kv_scale + (page * p.Hkv + kvh) * 32), 0, valid ? 128 : 0, kBufferFlags);
+                    const_cast<float *>(p.kv_scale + ((uint64_t)(uint32_t)entry * (uint32_t)p.Hkv + kvh) * 32), 0, entry < 0 ? 0 : 128, kBufferFlags);
                 in.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sd, c32 * 4, 0, 0));
             }
         };
         auto store = [&](int buf) {
-            if (N == 1 && wave >= 2) return;
-            unsigned char *ks = sh.k[buf], *vs = sh.v[buf];
+            unsigned char *ks = sh.k[buf] + (wave >> 1) * (KS * 1024) + (wave & 1) * 256, *vs = sh.v[buf];
 #pragma unroll
-            for (int i = 0; i < PN; ++i) {
-                const int j = j0 + 2 * i;
+            for (int j = 0; j < N; ++j) {
                 if constexpr (B8) {   // token n16, dims 64 j + 16 g .. + 15; tokens 4 g .. + 3, dims 64 j + 16 e + n16
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const u32x2 a = codes_to_bf16<INT8>(in.k[i][2 * e]), b = codes_to_bf16<INT8>(in.k[i][2 * e + 1]);
-                        *reinterpret_cast<u32x4 *>(ks + (4 * j + g) * 1024 + (e * 32 + my_page * 16 + n16) * 16) = (u32x4){a.x, a.y, b.x, b.y};
+                        const u32x2 a = codes_to_bf16<INT8>(in.k[j][2 * e]), b = codes_to_bf16<INT8>(in.k[j][2 * e + 1]);
+                        *reinterpret_cast<u32x4 *>(ks + (4 * j + g) * 1024 + (e * 32 + n16) * 16) = (u32x4){a.x, a.y, b.x, b.y};
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<u32x2 *>(vs + (my_page * SL + 2 * j + e / 2) * 1024 + ((g & 1) * 32 + (e % 2) * 16 + n16) * 16 + (g >> 1) * 8) =
-                            codes_to_f16<INT8>(in.v[i][e]);
+                        *reinterpret_cast<u32x2 *>(vs + (wave * SL + 2 * j + e / 2) * 1024 + ((g & 1) * 32 + (e % 2) * 16 + n16) * 16 + (g >> 1) * 8) =
+                            codes_to_f16<INT8>(in.v[j][e]);
                 } else {              // token n16, dims 32 j + 8 g .. + 7
-                    *reinterpret_cast<u32x4 *>(ks + (2 * j + (g >> 1)) * 1024 + ((g & 1) * 32 + my_page * 16 + n16) * 16) = in.k[i];
+                    *reinterpret_cast<u32x4 *>(ks + (2 * j + (g >> 1)) * 1024 + ((g & 1) * 32 + n16) * 16) = in.k[j];
                     if constexpr (TM) {
                         constexpr int LR = D / 8;   // lanes per token row of a 1 KB load
-                        *reinterpret_cast<u32x4 *>(vs + (my_page * SPEC_BLOCK_SIZE + (kWave / LR) * j + lane / LR) * v_row_bytes(D) + (lane % LR) * 16) = in.v[i];
+                        *reinterpret_cast<u32x4 *>(vs + (wave * SPEC_BLOCK_SIZE + (kWave / LR) * j + lane / LR) * v_row_bytes(D) + (lane % LR) * 16) = in.v[j];
                     } else {          // tokens 4 g .. + 3, dims 32 j + 16 e + n16
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
-                            *reinterpret_cast<u32x2 *>(vs + (my_page * SL + j) * 1024 + ((g & 1) * 32 + e * 16 + n16) * 16 + (g >> 1) * 8) =
-                                (u32x2){in.v[i][2 * e], in.v[i][2 * e + 1]};
+                            *reinterpret_cast<u32x2 *>(vs + (wave * SL + j) * 1024 + ((g & 1) * 32 + e * 16 + n16) * 16 + (g >> 1) * 8) =
+                                (u32x2){in.v[j][2 * e], in.v[j][2 * e + 1]};
                     }
                 }
             }
             if constexpr (B8) {
-                if (wave < 2 && lane < 32) {
-                    if (lane < 16) {
-                        sh.scale[buf][0][my_page * 16 + lane] = in.scale * p.scale_log2;
-                    } else {
-                        const float x = in.scale < kSmallestScale ? kSmallestScale : in.scale;   // (a page that reads as zeros)
-                        sh.scale[buf][1][my_page * 16 + lane - 16] = __builtin_amdgcn_logf(x);
-                        sh.scale[buf][2][my_page * 16 + lane - 16] = __builtin_amdgcn_rcpf(x);
+                if (lane < 32) {   // 16 scales of K, 16 of V (a page that reads as zeros: the smallest one)
+                    const float x = __builtin_elementwise_maximum(in.scale, kSmallestScale);
+                    float *to = &sh.scale[buf][0][wave * 16 + n16];
+                    constexpr int kRow = kStepPages * SPEC_BLOCK_SIZE;
+                    if (lane < 16) to[0] = in.scale * p.scale_log2;
+                    else {
+                        to[kRow] = __builtin_amdgcn_logf(x);
+                        to[2 * kRow] = __builtin_amdgcn_rcpf(x);
                     }
                 }
             }
@@ -1137,39 +1136,60 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[sl][e] = 0.0f;
 
-        f32x16 s;
-        Weights pw[2][TERMS];
+        f32x16 s[2];                 // of the step's pairs
+        Weights pw[2][2][TERMS];     // ... and their pages
+        // Operands come from LDS kAhead reads ahead of the products that take them.
+        constexpr int kAhead = 4;
+        u32x4 operand[kAhead];
+        auto read_k = [&](int buf, int i) { return *reinterpret_cast<const u32x4 *>(sh.k[buf] + i * 1024 + lane * 16); };   // pair i / KS, dims 16 (i % KS) ..
+        auto read_v = [&](int buf, int i) {   // page i / SL, dims 32 (i % SL) ..
+            if constexpr (TM) {
+                const unsigned char *src = sh.v[buf] + (i / SL * SPEC_BLOCK_SIZE + 4 * half + (n16 >> 2)) * v_row_bytes(D) + (i % SL * 32 + 16 * (g & 1) + 4 * (n16 & 3)) * 2;
+                const u32x2 a = read_transposed(src), b = read_transposed(src + 8 * v_row_bytes(D));
+                return (u32x4){a.x, a.y, b.x, b.y};
+            } else {
+                return *reinterpret_cast<const u32x4 *>(sh.v[buf] + i * 1024 + lane * 16);
+            }
+        };
         // products of the K in buffer `buf` with the queries
         auto scores = [&](int buf) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(sh.k[buf] + ks * 1024 + lane * 16), q[ks], s, 0, 0, 0);
+                for (int e = 0; e < 16; ++e) s[h][e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) {
+                s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand[i % kAhead]), q[i % KS], s[i / KS], 0, 0, 0);
+                if (i + kAhead < 2 * KS) operand[i % kAhead] = read_k(buf, i + kAhead);
+            }
         };
-        // scores to base-2 exponents (8-bit; bf16: up to the scale, which the exponent's multiply-add applies); the running reference
-        // raised where it has fallen behind; weights
-        auto weigh = [&](int buf, bool one_page) {
+        // scores to base-2 exponents (8-bit; bf16: up to the scale, which the exponent's multiply-add applies), and the running
+        // reference raised where it has fallen behind
+        auto exponents = [&](int buf, int pages) {
             if constexpr (B8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     const f32x4 ks = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][0][8 * i + 4 * half]);
                     const f32x4 lv = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][1][8 * i + 4 * half]);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[4 * i + r] = fmaf(s[4 * i + r], ks[r], lv[r]);
+                    for (int r = 0; r < 4; ++r) s[i / 4][4 * (i % 4) + r] = fmaf(s[i / 4][4 * (i % 4) + r], ks[r], lv[r]);
                 }
             }
-            if (one_page) {
+            if (pages < kStepPages) {
 #pragma unroll
-                for (int e = 8; e < 16; ++e) s[e] = -INFINITY;
+                for (int i = 1; i < kStepPages; ++i)
+                    if (i >= pages) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s[i / 2][8 * (i % 2) + e] = -INFINITY;
+                    }
             }
-            float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]);
-            a = max3(a, s[6], s[7]);
-            b = max3(b, s[8], s[9]);
-            a = max3(a, s[10], s[11]);
-            b = max3(b, s[12], s[13]);
-            a = max3(a, s[14], s[15]);
-            float mx = max3(a, b, b);
+            float mx = max3(s[0][0], s[0][1], s[0][2]), b = max3(s[1][0], s[1][1], s[1][2]);
+#pragma unroll
+            for (int e = 3; e < 15; e += 2) {
+                mx = max3(mx, s[0][e], s[0][e + 1]);
+                b = max3(b, s[1][e], s[1][e + 1]);
+            }
+            mx = max3(max3(mx, s[0][15], s[1][15]), b, b);
             mx = B8 ? mx - kTop : mx * p.scale_log2;   // (the scale is positive: the maximum commutes with it)
             const float limit = m_run + kRescaleSlack;
             if (__builtin_amdgcn_ballot_w64(mx > limit) != 0) {
@@ -1181,65 +1201,71 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
                 for (int sl = 0; sl < SL; ++sl) acc[sl] *= alpha;
                 m_run = m_new;
             }
+        };
+        // weights of pair h
+        auto weigh = [&](int buf, int h) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 f32x4 rv = {0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (B8) rv = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][2][8 * i + 4 * half]);
+                if constexpr (B8) rv = *reinterpret_cast<const f32x4 *>(&sh.scale[buf][2][32 * h + 8 * i + 4 * half]);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x = s[4 * i + r];
+                    const float x = s[h][4 * i + r];
                     const float e = fast_exp2(B8 ? x - m_run : fmaf(x, p.scale_log2, -m_run));
                     if constexpr (B8) l_run = fmaf(e, rv[r], l_run);
                     else if constexpr (FULL) l_run += e;
                     float rest = e;
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t) {
-                        pw[i / 2][t][4 * (i % 2) + r] = (std::conditional_t<B8, _Float16, __bf16>)rest;
-                        rest -= (float)pw[i / 2][t][4 * (i % 2) + r];
+                        pw[h][i / 2][t][4 * (i % 2) + r] = (std::conditional_t<B8, _Float16, __bf16>)rest;
+                        rest -= (float)pw[h][i / 2][t][4 * (i % 2) + r];
                     }
                 }
             }
             if constexpr (!B8 && !FULL) {   // the sum of the weights as they are multiplied, two at a time
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 8; e += 2)
-                        l_run = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pw[h][0][e], pw[h][0][e + 1]}, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, l_run, false);
+                        l_run = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pw[h][i][0][e], pw[h][i][0][e + 1]}, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, l_run, false);
             }
         };
-        // the weights' product with the V in buffer `buf`
-        auto product = [&](int buf) {
-            const unsigned char *v0 = sh.v[buf];
+        // product of pair h's weights with its V in buffer `buf`
+        auto product = [&](int buf, int h) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int k = 0; k < 2 * SL; ++k) {
+                const int i = 2 * SL * h + k;
+                const u32x4 v = operand[i % kAhead];
 #pragma unroll
-                for (int sl = 0; sl < SL; ++sl) {
-                    u32x4 v;
-                    if constexpr (TM) {
-                        const unsigned char *src = v0 + (h * SPEC_BLOCK_SIZE + 4 * half + (n16 >> 2)) * v_row_bytes(D) + (32 * sl + 16 * (g & 1) + 4 * (n16 & 3)) * 2;
-                        const u32x2 a = read_transposed(src), b = read_transposed(src + 8 * v_row_bytes(D));
-                        v = (u32x4){a.x, a.y, b.x, b.y};
-                    } else {
-                        v = *reinterpret_cast<const u32x4 *>(v0 + (h * SL + sl) * 1024 + lane * 16);
-                    }
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) {
-                        if constexpr (B8) acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, pw[h][t]), acc[sl], 0, 0, 0);
-                        else acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pw[h][t]), acc[sl], 0, 0, 0);
-                    }
+                for (int t = 0; t < TERMS; ++t) {
+                    const Weights w8 = pw[h][k / SL][t];
+                    if constexpr (B8) acc[k % SL] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, w8), acc[k % SL], 0, 0, 0);
+                    else acc[k % SL] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w8), acc[k % SL], 0, 0, 0);
                 }
+                if (i + kAhead < 4 * SL) operand[i % kAhead] = read_v(buf, i + kAhead);
+            }
         };
 
-        load(0);
+        load(sh.page[wave]);
         store(0);
-        load(1);
-        for (int u = 0; u < pairs; ++u) {
-            __syncthreads();        // pair u is in LDS, and no wavefront reads pair u - 1 any more
-            store((u + 1) & 1);
-            load(u + 2);
-            scores(u & 1);
-            weigh(u & 1, u == pairs - 1 && last_pages == 1);
-            product(u & 1);
+        load(sh.page[kStepPages + wave]);
+        int entry_ahead = sh.page[2 * kStepPages + wave];
+        for (int u = 0; u < steps; ++u) {
+            const int buf = u & 1;
+            __syncthreads();        // step u is in LDS, and no wavefront reads step u - 1 any more
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) operand[i] = read_k(buf, i);
+            store(buf ^ 1);
+            load(entry_ahead);
+            entry_ahead = sh.page[kStepPages * (u + 3) + wave];
+            scores(buf);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) operand[i] = read_v(buf, i);
+            exponents(buf, u == steps - 1 ? last_pages : kStepPages);
+            weigh(buf, 0);
+            product(buf, 0);
+            weigh(buf, 1);
+            product(buf, 1);
         }
 
         // The rows' partial results, half of the dims at a time through LDS so that they go out in long pieces.
@@ -1298,7 +1324,7 @@ __global__ __launch_bounds__(kThreads, 3) void prefix_rows_kernel(CacheAttnParam
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
-        pos += pairs;
+        pos += steps;
     }
 }
 

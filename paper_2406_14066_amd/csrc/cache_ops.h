@@ -51,7 +51,8 @@ hipError_t launch_kv8_read(const Kv8ReadParams &p, hipStream_t stream);
 constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's four wavefronts: 64 pages each
 
 constexpr int kPrefixRows = 128;        // many rows: rows of a row block
-constexpr int kMaxPrefixPairs = 128;    // ... and most steps (pairs of pages) of a block
+constexpr int kStepPages = 4;           // ... pages of a step
+constexpr int kMaxPrefixSteps = 64;     // ... most steps of a block
 
 struct CacheAttnParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, G;

@@ -87,13 +87,18 @@ __device__ __forceinline__ int request_of(const int32_t *cu, int B, int row, int
 // enough for n = cu[b+1] - cu[b] tokens from any position: those touch at most n / 16 + 2 pages.
 __host__ __device__ __forceinline__ int page_item(int packed, int b) { return packed / SPEC_BLOCK_SIZE + 2 * b; }
 
-__device__ __forceinline__ int request_of_item(const int32_t *cu, int B, int item, int guess)
+// The request that owns an item: the last one whose first item is not beyond it.  A wavefront asks 64 places at a time (256 requests:
+// two loads one after another, where halving takes eight).
+__device__ __forceinline__ int request_of_item(const int32_t *cu, int B, int item)
 {
-    if (page_item(cu[guess], guess) <= item && item < page_item(cu[guess + 1], guess + 1)) return guess;
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (page_item(cu[mid], mid) <= item) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x % kWave;
+    int lo = 0, n = B;
+    while (n > 1) {
+        const int stride = (n + kWave - 1) / kWave, at = lo + lane * stride;
+        const bool begun = lane * stride < n && page_item(cu[min(at, B - 1)], at) <= item;
+        const int count = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(begun)), 1);
+        lo += (count - 1) * stride;
+        n = min(stride, n - (count - 1) * stride);
     }
     return lo;
 }

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
     if (item >= items) return;   // (the wavefronts of a block are independent)
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
-    w.b = request_of_item(p.cu_q_len, p.B, item, min((int)((int64_t)item * p.B / items), p.B - 1));
+    w.b = request_of_item(p.cu_q_len, p.B, item);
     const int row0 = p.cu_q_len[w.b], n = p.cu_q_len[w.b + 1] - row0;
     if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
     const int pos0 = p.kv_len[w.b] - n;
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_read_kernel(Kv8ReadPara
     if (item >= items) return;   // (the wavefronts of a block are independent)
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
-    w.b = request_of_item(p.cu_len, p.B, item, min((int)((int64_t)item * p.B / items), p.B - 1));
+    w.b = request_of_item(p.cu_len, p.B, item);
     const int row0 = p.cu_len[w.b], n = p.cu_len[w.b + 1] - row0;
     if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
     const int pos0 = p.start != nullptr ? p.start[w.b] : 0;
