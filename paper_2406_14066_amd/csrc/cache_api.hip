@@ -151,7 +151,7 @@ constexpr int kMostTiles = 3;   // row tiles of a block
 
 struct Plan {
     int row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
-    int prefix_tiles, prefix_many_rows, prefix_block_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
+    int prefix_tiles, prefix_many_rows, prefix_piece_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
     size_t acc, ml, tickets, prefix_acc, prefix_ml, total;   // offsets into the workspace
     int64_t blocks, prefix_blocks;
 };
@@ -203,17 +203,38 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double tick
     return best;
 }
 
-// Steps of a block of the launch for prefixes with many rows: three blocks on each compute unit, which is what fits, and keeps
-// matrix cores and vector units busy at the same time (64 requests behind 4096 tokens, 64/8 heads, k = 2, bf16: one, two, three
-// blocks 62.7 / 51.5 / 44.6 us), unless that leaves a block fewer than 12 steps: then one on each, since every block
-// leaves partial results to write and to read back (11 steps a unit, d = 64, fp32 output: 21.2 + 17.3 us for this launch and the one
-// after it, 19.2 + 25.0 with three).
-int prefix_block_steps(int64_t steps)
+// Most steps of a piece of the launch for prefixes with many rows, from a model of it.  A block takes kPieceUs besides its steps; a step
+// takes kStepUs while the block has its compute unit for itself, and kSharedStepUs where two share one, which is what fits: matrix cores and
+// vector units are busy at the same time more often (d = 128, weights in one term; measured behind one prefix of 4096 tokens, 64
+// requests, 64/8 heads, k = 2: 24 steps alone 32 us, 12 and 12 together 22 us).  More blocks than that take turns.  Each piece of a prefix is
+// partial results to write and to read back.
+constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kPieceJoinUs = 0.35;
+template <typename F>
+int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, F for_each_group)   // for_each_group(f): f(row blocks, steps)
 {
-    const int64_t units = compute_units();
-    const int64_t slots = steps >= 2 * units * 6 ? 2 * units : units;
-    const int64_t rounds = (steps + slots * kMaxPrefixSteps - 1) / (slots * kMaxPrefixSteps);
-    return (int)std::max<int64_t>((steps + slots * rounds - 1) / (slots * rounds), 1);
+    const double units = compute_units(), factor = d / 128.0 * (full ? (codes ? 1.5 : 2.0) : 1.0);   // (more terms: more products with V)
+    int best = std::min(most_steps, kMaxPrefixSteps);
+    double best_us = 1e30;
+    for (int len = best; len >= 1; len = std::min(len - 1, len * 7 / 8)) {
+        double count = 0.0, sum = 0.0, longest = 0.0, pieces = 0.0;
+        for_each_group([&](int64_t row_blocks, int steps) {
+            if (steps == 0) return;
+            const int n = (steps + len - 1) / len, each = (steps + n - 1) / n;
+            count += (double)row_blocks * n * Hkv;
+            sum += (double)row_blocks * n * Hkv * (kPieceUs + each * kSharedStepUs * factor);
+            longest = std::max(longest, (double)each);
+            pieces = std::max(pieces, (double)n);
+        });
+        double us = kPieceUs + longest * factor * (count <= units ? kStepUs : kSharedStepUs);
+        if (count > 2 * units) us = std::max(us, sum / (2 * units) + 0.5 * longest * factor * kSharedStepUs);
+        us += pieces * kPieceJoinUs;
+        if (us < best_us) {
+            best_us = us;
+            best = len;
+        }
+        if (sum / (2 * units) > best_us) break;   // (shorter pieces are more work in all)
+    }
+    return best;
 }
 
 Plan make_plan(const spec_prefix_attn_args *a)
@@ -262,15 +283,17 @@ Plan make_plan(const spec_prefix_attn_args *a)
         auto rows_of = [&](int g) { return (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group; };
         if (pl.prefix_many_rows) {
             constexpr int kStepTokens = kStepPages * SPEC_BLOCK_SIZE;
-            auto walk_of = [&](int tokens) { return (tokens + kStepTokens - 1) / kStepTokens; };
-            int64_t steps = 0;
-            for (int g = 0; g < a->G; ++g) steps += (rows_of(g) + kPrefixRows - 1) / kPrefixRows * walk_of(a->host_prefix_len[g]);
-            steps *= a->Hkv;
-            pl.prefix_block_steps = prefix_block_steps(steps);
-            pl.prefix_blocks = ((steps + pl.prefix_block_steps - 1) / pl.prefix_block_steps + kXcdCount - 1) / kXcdCount * kXcdCount;
-            pl.prefix_row_blocks = (int)pl.prefix_blocks;
-            // partial results of a row block: one of each block that its steps touch
-            pl.max_prefix_chunks = (walk_of(max_prefix) + pl.prefix_block_steps - 2) / pl.prefix_block_steps + 1;
+            auto steps_of = [&](int tokens) { return (tokens + kStepTokens - 1) / kStepTokens; };
+            auto each_group = [&](auto group) {
+                for (int g = 0; g < a->G; ++g) group((rows_of(g) + kPrefixRows - 1) / kPrefixRows, steps_of(a->host_prefix_len[g]));
+            };
+            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, each_group);
+            each_group([&](int64_t row_blocks, int steps) {
+                pl.prefix_blocks += row_blocks * ((steps + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps) * a->Hkv;
+            });
+            pl.prefix_blocks = (pl.prefix_blocks + kXcdCount - 1) / kXcdCount * kXcdCount;
+            pl.prefix_row_blocks = (int)std::min<int64_t>(pl.prefix_blocks, INT32_MAX);
+            pl.max_prefix_chunks = (steps_of(max_prefix) + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps;
         } else {
             const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, full, 0.0, [&](auto job) {   // (no ticket: the next launch joins)
                 for (int g = 0; g < a->G; ++g)
@@ -312,8 +335,8 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
 {
     const Plan pl = make_plan(a);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
-    if (a->B > 65535 || pl.prefix_row_blocks > 65535 || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
-    if (pl.blocks > kMaxPacked || pl.prefix_blocks * std::max(pl.prefix_block_steps, 1) > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if (a->B > 65535 || (!pl.prefix_many_rows && pl.prefix_row_blocks > 65535) || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
+    if (pl.blocks > kMaxPacked || pl.prefix_blocks > kMaxPacked) return SPEC_EUNSUPPORTED;
     char *ws = static_cast<char *>(workspace);
     CacheAttnParams p;
     memset(&p, 0, sizeof p);
@@ -325,7 +348,7 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     p.out_f32 = a->out_dtype == SPEC_F32;
     p.row_tiles = pl.row_tiles; p.row_blocks = pl.row_blocks; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks;
     p.capacity_tokens = pl.capacity; p.max_q_rows = pl.max_q_rows;
-    p.prefix_tiles = pl.prefix_tiles; p.prefix_many_rows = pl.prefix_many_rows; p.prefix_block_steps = pl.prefix_block_steps; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
+    p.prefix_tiles = pl.prefix_tiles; p.prefix_many_rows = pl.prefix_many_rows; p.prefix_piece_steps = pl.prefix_piece_steps; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
     p.max_prefix_chunks = pl.max_prefix_chunks; p.prefix_capacity = pl.prefix_capacity;
     p.generation = next_generation();
     p.group_inverse = (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group);   // (unused where the group is 1)

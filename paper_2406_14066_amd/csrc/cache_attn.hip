@@ -97,8 +97,6 @@ struct Work {
     int group_index, first_of_group, end_of_group;    // its group, and (lane-wise, groups 0 .. 63) every group's requests and prefix
     int prefix_of_group;
     int prefix_chunks;                // partial results that come in from the prefix launch
-    int prefix_base, prefix_walk;    // ... with many rows: the group's first step on this KV head, the steps of a row block
-    int prefix_row0;                  // ... and its first packed token row
     int row_block;
 };
 
@@ -143,90 +141,58 @@ __device__ __forceinline__ bool prefix_ok(const CacheAttnParams &p, int len)
 
 __device__ __forceinline__ int chunk_count(int tokens, int chunk_tokens) { return (tokens + chunk_tokens - 1) / chunk_tokens; }
 
-// Steps of the launch for prefixes with many query rows (see prefix_rows_kernel): of all groups of a KV head in `total`,
-// of the groups before group `upto` as the result.
-__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int b0, int b1, int P, int &walk, int &rows, int &row0)
-{
-    walk = rows = row0 = 0;
-    if (b0 < 0 || b0 > b1 || b1 > p.B || !prefix_ok(p, P)) return 0;
-    row0 = p.cu_q_len[b0];
-    const int end = p.cu_q_len[b1];
-    rows = (end - row0) * p.group;
-    if (row0 < 0 || end > p.T || rows <= 0) return 0;
-    walk = (P + kStepPages * SPEC_BLOCK_SIZE - 1) / (kStepPages * SPEC_BLOCK_SIZE);
-    return (rows + kPrefixRows - 1) / kPrefixRows * walk;
-}
+// A group of the launch for prefixes with many query rows (see prefix_rows_kernel): its row blocks, and the pieces that each of
+// them walks the prefix in.
+struct GroupWork {
+    int request, row0, rows, pages;   // first request, first packed token row, fused query rows, pages of the prefix
+    int pieces, blocks;               // ... row blocks times pieces: the blocks of a KV head; 0: none (or not valid, which the own launch reports)
+    __device__ __forceinline__ void set(const CacheAttnParams &p, int b0, int b1, int P)
+    {
+        request = row0 = rows = pages = pieces = blocks = 0;
+        if (b0 < 0 || b0 > b1 || b1 > p.B || !prefix_ok(p, P)) return;
+        request = b0;
+        row0 = p.cu_q_len[b0];
+        const int end = p.cu_q_len[b1];
+        rows = (end - row0) * p.group;
+        if (row0 < 0 || end > p.T || rows <= 0) return;
+        pages = P / SPEC_BLOCK_SIZE;
+        const int steps = (pages + kStepPages - 1) / kStepPages;
+        pieces = (steps + p.prefix_piece_steps - 1) / p.prefix_piece_steps;
+        blocks = (rows + kPrefixRows - 1) / kPrefixRows * pieces;
+    }
+    __device__ __forceinline__ void look(const CacheAttnParams &p, int g)
+    {
+        if (g < p.G) set(p, p.cu_group[g], p.cu_group[g + 1], p.prefix_len[g]);
+        else request = row0 = rows = pages = pieces = blocks = 0;
+    }
+};
 
-__device__ __forceinline__ int group_steps(const CacheAttnParams &p, int g, int &walk, int &rows)
-{
-    int row0;
-    return group_steps(p, p.cu_group[g], p.cu_group[g + 1], p.prefix_len[g], walk, rows, row0);
-}
-
-__device__ __forceinline__ int prefix_steps(const CacheAttnParams &p, int upto, int &total)
+// The sum over the lanes, and over this lane and those before it.
+__device__ __forceinline__ int running_sum(int x, int &all)
 {
     const int lane = threadIdx.x % kWave;
-    int all = 0, before = 0;
-    for (int base = 0; base < p.G; base += kWave) {
-        int walk, rows, n = base + lane < p.G ? group_steps(p, base + lane, walk, rows) : 0;
-        int some = base + lane < upto ? n : 0;
 #pragma unroll
-        for (int off = kWave / 2; off > 0; off >>= 1) {
-            n += __shfl_xor(n, off);
-            some += __shfl_xor(some, off);
-        }
-        all += n;
-        before += some;
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int up = __shfl_up(x, off);
+        if (lane >= off) x += up;
     }
-    total = __builtin_amdgcn_readfirstlane(all);
-    return __builtin_amdgcn_readfirstlane(before);
+    all = __builtin_amdgcn_readlane(x, kWave - 1);
+    return x;
 }
 
-struct PrefixPlace {
-    int request, row0, rows;    // the group's first request, its first packed token row, its fused query rows
-    int row_block, first;       // row block of the step, and which of its steps it is
-    int walk, pages;            // steps of a row block, pages of the prefix
-};
-
-// The groups base .. base + 63, a lane each.
-struct GroupLanes {
-    int b0, pages, row0, rows, walk;
-    int steps, upto;   // of the group; of it and the lanes before it
-    __device__ __forceinline__ void look(const CacheAttnParams &p, int base)
-    {
-        const int lane = threadIdx.x % kWave, g = base + lane;
-        steps = b0 = pages = row0 = rows = walk = 0;
-        if (g < p.G) {
-            b0 = p.cu_group[g];
-            const int b1 = p.cu_group[g + 1], P = p.prefix_len[g];
-            steps = group_steps(p, b0, b1, P, walk, rows, row0);
-            pages = P / SPEC_BLOCK_SIZE;
-        }
-        upto = steps;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const int up = __shfl_up(upto, off);
-            if (lane >= off) upto += up;
-        }
+// Blocks of a KV head, all groups.
+__device__ __forceinline__ int group_blocks(const CacheAttnParams &p)
+{
+    int total = 0;
+    for (int base = 0; base < p.G; base += kWave) {
+        GroupWork work;
+        work.look(p, base + threadIdx.x % kWave);
+        int all;
+        (void)running_sum(work.blocks, all);
+        total += all;
     }
-    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, kWave - 1); }
-    // step `step`, counted from these groups' first; false: it lies after them
-    __device__ __forceinline__ bool find(int step, PrefixPlace &at) const
-    {
-        const unsigned long long holds = __builtin_amdgcn_ballot_w64(upto > step);
-        if (holds == 0) return false;
-        const int who = __builtin_ctzll(holds);
-        const int rest = step - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(steps, who));
-        at.walk = __builtin_amdgcn_readlane(walk, who);
-        at.rows = __builtin_amdgcn_readlane(rows, who);
-        at.row0 = __builtin_amdgcn_readlane(row0, who);
-        at.request = __builtin_amdgcn_readlane(b0, who);
-        at.pages = __builtin_amdgcn_readlane(pages, who);
-        at.row_block = rest / at.walk;
-        at.first = rest - at.row_block * at.walk;
-        return true;
-    }
-};
+    return total;
+}
 
 // One block of the own launch: grid (KV heads, requests, row blocks x chunks).
 template <int NT>
@@ -290,40 +256,32 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
 __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w)
 {
     w.prefix_chunks = 0;
-    w.prefix_walk = 0;
     if (w.prefix == 0) return true;
     if (!p.prefix_many_rows) {
         w.prefix_chunks = chunk_count(w.prefix, p.prefix_chunk_tokens);
         return true;
     }
-    int total, before, rows;
+    GroupWork work;
+    int total, rows, row0;
     if (p.G <= kWave) {
-        const int lane = threadIdx.x % kWave;
-        int walk = 0, all_rows = 0, row0 = 0;
-        int n = lane < p.G ? group_steps(p, w.first_of_group, w.end_of_group, w.prefix_of_group, walk, all_rows, row0) : 0;
-        int some = lane < w.group_index ? n : 0;
-        w.prefix_walk = __builtin_amdgcn_readlane(n, w.group_index) > 0 ? __builtin_amdgcn_readlane(walk, w.group_index) : 0;
-        rows = __builtin_amdgcn_readlane(all_rows, w.group_index);
-        w.prefix_row0 = __builtin_amdgcn_readlane(row0, w.group_index);
-#pragma unroll
-        for (int off = kWave / 2; off > 0; off >>= 1) {
-            n += __shfl_xor(n, off);
-            some += __shfl_xor(some, off);
-        }
-        total = __builtin_amdgcn_readfirstlane(n);
-        before = __builtin_amdgcn_readfirstlane(some);
+        if ((int)(threadIdx.x % kWave) < p.G) work.set(p, w.first_of_group, w.end_of_group, w.prefix_of_group);
+        else work.look(p, p.G);
+        (void)running_sum(work.blocks, total);
+        w.prefix_chunks = __builtin_amdgcn_readlane(work.pieces, w.group_index);
+        rows = __builtin_amdgcn_readlane(work.rows, w.group_index);
+        row0 = __builtin_amdgcn_readlane(work.row0, w.group_index);
     } else {
-        before = prefix_steps(p, w.group_index, total);
-        if (group_steps(p, w.group_index, w.prefix_walk, rows) == 0) w.prefix_walk = 0;
-        w.prefix_row0 = w.prefix_walk > 0 ? uniform_load(p.cu_q_len, uniform_load(p.cu_group, w.group_index)) : 0;
+        total = group_blocks(p);
+        work.look(p, w.group_index);
+        w.prefix_chunks = __builtin_amdgcn_readfirstlane(work.pieces);
+        rows = __builtin_amdgcn_readfirstlane(work.rows);
+        row0 = __builtin_amdgcn_readfirstlane(work.row0);
     }
-    const int after = (w.row0 - w.prefix_row0) * p.group;   // the request's rows lie in its group's
-    if ((int64_t)total * p.Hkv > (int64_t)p.prefix_row_blocks * p.prefix_block_steps || w.prefix_walk == 0 || after < 0 ||
-        after + w.rows > rows) {
+    const int after = (w.row0 - row0) * p.group;   // the request's rows lie in its group's
+    if ((int64_t)total * p.Hkv > p.prefix_row_blocks || w.prefix_chunks == 0 || after < 0 || after + w.rows > rows) {
         count_error(p, w.chunk == 0 && w.kvh == 0 && w.row_block == 0);
         return false;
     }
-    w.prefix_base = w.kvh * total + before;
     return true;
 }
 
@@ -506,14 +464,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     load_scales(0);
     load_v(0);
     if (!place_partials(p, w)) return;
-    // Partial results of the block's row r: those of the blocks from the one that took the first step of its row block to the one that
-    // took the last (many rows), or one of each chunk.
-    auto partials_of = [&](int r) {
-        if (w.prefix_walk == 0) return w.prefix_chunks;
-        const int rr = (w.row0 - w.prefix_row0) * p.group + w.row_lo + r;
-        const int step = w.prefix_base + rr / kPrefixRows * w.prefix_walk;
-        return (step + w.prefix_walk - 1) / p.prefix_block_steps - step / p.prefix_block_steps + 1;
-    };
 #pragma unroll
     for (int k = 0; k < QN; ++k) {
         const int piece = k * kThreads + tid;
@@ -876,24 +826,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         }
     }
     // the prefix's partial results
-    int pieces[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) pieces[nt] = partials_of(min(nt * 16 + n16, rows - 1));
     if (w.prefix > 0) {
-        int most = 0;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) most = max(most, pieces[nt]);
+        const bool many = p.prefix_many_rows != 0;
         auto add_pieces = [&](auto count, int c0) {
             constexpr int U = decltype(count)::value;
             f32x2 ml[NT][U];
             u32x4 o[NT][U][SN];   // as they were stored
             constexpr int kHalves = SN == 2 ? 1 : 0;   // (fp16: a lane's two slices are 16 bytes)
-            const bool halves = !FULL && w.prefix_walk > 0;
+            const bool halves = !FULL && many;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, pieces[nt] - 1);
+                    const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, w.prefix_chunks - 1);
                     ml[nt][u] = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
                     if (halves) {
                         const _Float16 *from = reinterpret_cast<const _Float16 *>(p.prefix_acc) + slot * D + partial_place<D>(dim0);
@@ -907,7 +852,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                         const float *from = p.prefix_acc + slot * D;
 #pragma unroll
                         for (int i = 0; i < SN; ++i)
-                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (w.prefix_walk > 0 ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
+                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (many ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
                     }
                 }
 #pragma unroll
@@ -923,11 +868,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 #pragma unroll
                         for (int i = 0; i < SN; ++i) x[i] = __builtin_bit_cast(f32x4, o[nt][u][i]);
                     }
-                    if (c0 + u < pieces[nt]) sum[nt].add(ml[nt][u].x, ml[nt][u].y, x);
+                    if (c0 + u < w.prefix_chunks) sum[nt].add(ml[nt][u].x, ml[nt][u].y, x);
                 }
         };
-        for (int c0 = 0; __builtin_amdgcn_ballot_w64(c0 < most) != 0;) {
-            if (__builtin_amdgcn_ballot_w64(c0 + kFew < most) != 0) {
+        for (int c0 = 0; c0 < w.prefix_chunks;) {
+            if (w.prefix_chunks - c0 > kFew) {
                 add_pieces(std::integral_constant<int, kMany>(), c0);
                 c0 += kMany;
             } else {
@@ -955,10 +900,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 // ---------------------------------------------------------------------------
 // Prefixes of groups with many query rows.
 //
-// The work is counted in (row block of 128 rows, four pages) steps, laid out KV head by KV head, group by group, row block
-// by row block; every block takes the same number of consecutive steps, whatever row blocks they belong to, and leaves a
-// partial result for each row block it touches.  So all blocks end together however ragged the groups are, and the blocks
-// of an XCD share their KV heads' pages in its L2.
+// A block takes a row block of 128 rows through a piece of its group's prefix, counted in steps of four pages: the pieces of a prefix are
+// as even as they can be, and at most so long that the blocks of all groups fill the device (the host's choice).  Blocks lie KV head by KV
+// head, group by group, row block by row block, and consecutive ones on one XCD, which share their KV head's pages in its L2.
 //
 // A block's four wavefronts have 32 rows each and walk the same pages, which pass through LDS once for all of them, a step
 // (64 tokens, a page brought in by each wavefront) at a time.  In LDS the pages lie as the operands of v_mfma_f32_32x32x16 want
@@ -986,7 +930,6 @@ struct RowsShared {
     float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? kStepPages * SPEC_BLOCK_SIZE : 1];
     int page[kStepPages * (kMaxPrefixSteps + 4)];   // the steps' block-table entries, and four more steps'; -1: outside the pool, or past the end
     static_assert(kStepPages * kMaxPrefixSteps == kThreads, "a thread per page");
-    GroupLanes groups[kWave];
 };
 
 template <int KIND, int D, bool FULL>
@@ -1007,45 +950,48 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
     // consecutive blocks go to different XCDs; consecutive steps stay on one
     const int block = (int)(blockIdx.x % kXcdCount) * (gridDim.x / kXcdCount) + blockIdx.x / kXcdCount;
 
-    // the first 64 groups, kept in LDS (the walk needs the registers)
-    int total;   // steps of a KV head
-    {
-        GroupLanes groups;
-        groups.look(p, 0);
-        total = groups.total();
-        if (wave == 0) sh.groups[lane] = groups;
+    // the group, row block and piece
+    int total = 0, rest = block, first = 0, steps = 0, row_block = 0;   // blocks of a KV head; its how-many-th block; the piece
+    GroupWork work;
+    work.look(p, lane);
+    int all, upto = running_sum(work.blocks, all);
+    total = p.G > kWave ? group_blocks(p) : all;
+    if (total == 0 || (int64_t)total * p.Hkv > gridDim.x) return;   // (not the groups planned for: the own launch reports it)
+    const int kvh = block / total;
+    if (kvh >= p.Hkv) return;
+    rest -= kvh * total;
+    for (int base = kWave; rest >= all; base += kWave) {   // (more than 64 groups; rest < total)
+        rest -= all;
+        work.look(p, base + lane);
+        upto = running_sum(work.blocks, all);
     }
-    if (p.G > kWave) prefix_steps(p, -1, total);
-    if ((int64_t)total * p.Hkv > (int64_t)gridDim.x * p.prefix_block_steps) return;   // (not the groups planned for: the own launch reports it)
-    int pos = block * p.prefix_block_steps;
-    const int end = min(pos + p.prefix_block_steps, total * p.Hkv);
-    __syncthreads();   // the groups are in LDS
-
-    while (pos < end) {
-        // the row block that step `pos` belongs to
-        const int kvh = pos / total;
-        PrefixPlace at = {};
-        int step = pos - kvh * total;
-        for (int base = 0; base < p.G; base += kWave) {
-            GroupLanes groups;
-            if (base == 0) groups = sh.groups[lane];
-            else groups.look(p, base);
-            if (groups.find(step, at)) break;
-            step -= groups.total();
-        }
-        const int steps = min(at.walk - at.first, end - pos);
-        const int slot = block - (pos - at.first) / p.prefix_block_steps;
-        const int row0 = at.row0;                                   // the group's first packed token row
-        const int row_lo = at.row_block * kPrefixRows + wave * 32;
-        const int rows = min(max(at.rows - row_lo, 0), 32);         // this wavefront's
-        auto out_index = [&](int r) {
-            return packed_row(p, row0, kvh, row_lo + r);
-        };
-        __syncthreads();   // (the previous row block's results have left LDS)
-        const bool used = tid < kStepPages * steps && tid < at.pages - kStepPages * at.first;   // pages from the first one of these steps on
+    {
+        const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > rest));
+        rest -= __builtin_amdgcn_readlane(upto - work.blocks, who);
+        work.request = __builtin_amdgcn_readlane(work.request, who);
+        work.row0 = __builtin_amdgcn_readlane(work.row0, who);
+        work.rows = __builtin_amdgcn_readlane(work.rows, who);
+        work.pages = __builtin_amdgcn_readlane(work.pages, who);
+        work.pieces = __builtin_amdgcn_readlane(work.pieces, who);
+    }
+    row_block = rest / work.pieces;
+    const int slot = rest - row_block * work.pieces;
+    {
+        const int all_steps = (work.pages + kStepPages - 1) / kStepPages, each = (all_steps + work.pieces - 1) / work.pieces;
+        first = slot * each;
+        steps = min(all_steps - first, each);
+    }
+    const int row0 = work.row0;                                 // the group's first packed token row
+    const int row_lo = row_block * kPrefixRows + wave * 32;
+    const int rows = min(max(work.rows - row_lo, 0), 32);       // this wavefront's
+    auto out_index = [&](int r) {
+        return packed_row(p, row0, kvh, row_lo + r);
+    };
+    {
+        const bool used = tid < kStepPages * steps && tid < work.pages - kStepPages * first;   // pages from the first one of these steps on
         int entry = -1;
-        if (used) entry = p.block_table[(size_t)at.request * p.max_blocks_per_req + kStepPages * at.first + tid];
-        const int last_pages = at.pages - kStepPages * (at.first + steps - 1);   // of the last step: 1 .. 4 (or more follow)
+        if (used) entry = p.block_table[(size_t)work.request * p.max_blocks_per_req + kStepPages * first + tid];
+        const int last_pages = work.pages - kStepPages * (first + steps - 1);   // of the last step: 1 .. 4 (or more follow)
         bf16x8 q[KS];
         {
             const __bf16 *row = query_row(p, row0, kvh, c32 < rows ? row_lo + c32 : 0);
@@ -1057,7 +1003,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             sh.page[tid] = bad ? -1 : entry;
             if (tid < 4 * kStepPages) sh.page[kThreads + tid] = -1;
             const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
-            if (bad_lanes != 0 && kvh == 0 && at.row_block == 0 && lane == 0 && p.errors != nullptr)
+            if (bad_lanes != 0 && kvh == 0 && row_block == 0 && lane == 0 && p.errors != nullptr)
                 atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
         }
         __syncthreads();
@@ -1324,7 +1270,6 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
-        pos += steps;
     }
 }
 

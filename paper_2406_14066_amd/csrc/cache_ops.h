@@ -62,7 +62,7 @@ struct CacheAttnParams {
     int32_t capacity_tokens;                    // longest kv_len planned for
     int32_t prefix_tiles, prefix_row_blocks;    // prefix: 16-row tiles of a block, blocks over all groups
     int32_t prefix_chunk_tokens, max_prefix_chunks;   // 0: no group has a prefix
-    int32_t prefix_many_rows, prefix_block_steps;   // the launch for many rows: steps of a block, prefix_row_blocks blocks
+    int32_t prefix_many_rows, prefix_piece_steps;   // the launch for many rows: steps of a block, prefix_row_blocks blocks
     int32_t prefix_capacity;                    // longest prefix planned for
     int32_t max_q_rows;                         // rows of the largest request
     uint32_t generation;
