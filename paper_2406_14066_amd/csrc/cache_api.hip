@@ -150,7 +150,7 @@ spec_status check_attn(const spec_prefix_attn_args *a)
 constexpr int kMostTiles = 3;   // row tiles of a block
 
 struct Plan {
-    int row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
+    int whole_context, row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
     int prefix_tiles, prefix_many_rows, prefix_piece_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
     size_t acc, ml, tickets, prefix_acc, prefix_ml, total;   // offsets into the workspace
     int64_t blocks, prefix_blocks;
@@ -167,21 +167,33 @@ struct Plan {
 // unit end at different times, which costs half of the longest one.
 struct Split {
     int tiles, length;
+    double us;
 };
 constexpr double kBlockUs[4] = {0.0, 4.7, 5.5, 6.7}, kTokenUs[4] = {0.0, 0.0052, 0.0064, 0.0078};
-constexpr double kFullFactor = 1.4;                                                  // of a token, with weights in more than one term
+constexpr double kFullFactor = 1.4, kShortFactor = 0.7;                              // of a token, with weights in more than one term; with d = 64
 constexpr double kTicketUs = 2.5, kJoinUs[4] = {0.0, 0.55, 0.75, 0.95};              // of a split job; of each of its chunks
 constexpr double kSecondBlock = 1.1;
+
+// A prefix is walked once for all of its group's rows by a launch of its own, whose results the own launch takes in; or each request
+// walks its whole context, which is one launch and reads the prefix again for every request, mostly from the caches.  The second is
+// less work than it seems while prefixes are short or groups small (64/8 heads, bf16 pages: two requests behind 512 tokens 13.1 -> 8.2 us, 64
+// behind 512 tokens 35 -> 18; 32/8 heads, 8-bit, 4 x 16 requests behind 2048 tokens 40 -> 29), the first where they are long
+// and groups large (64/8 heads, 64 requests behind 4096 tokens 69 against 87; 32/8 heads, 2 x 64 behind 8192 123 against 273; 16 x 12
+// requests without drafts behind 8192 125 against 499).  The model of the second: a token that comes from the caches costs a busy compute
+// unit kCachedTokens of its time alone, kFarTokens of it when the prefixes of a KV head do not fit an XCD's L2 well (kNearBytes) or
+// are bf16, twice the bytes; it was found too low by kWhole*; and the caches give kCacheBytesPerUs.  Of the first: the sum of its launches
+// was found too low by kTwoLaunches, and memory gives kMemoryBytesPerUs.
+constexpr double kCachedTokens = 0.5, kFarTokens = 0.7, kNearBytes = 3e6, kWholeBf16 = 1.15, kWholeInt8 = 1.25, kCacheBytesPerUs = 9e6;
+constexpr double kTwoLaunches = 1.1, kLaunchUs = 2.5, kMemoryBytesPerUs = 5.3e6;
 template <typename F>
-Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double ticket_us, F for_each_job)   // for_each_job(f): f(tokens, rows)
+Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, double ticket_us, double busy_tokens, F for_each_job)   // for_each_job(f): f(tokens, rows)
 {
     const int most = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
     const double units = compute_units();
     const int most_tiles = std::min((most_rows + 15) / 16, kMostTiles);
-    Split best = {most_tiles, most};
-    double best_us = 1e30;
+    Split best = {most_tiles, most, 1e30};
     for (int tiles = most_tiles; tiles >= 1; --tiles) {
-        const double token_us = kTokenUs[tiles] * (full ? kFullFactor : 1.0);
+        const double token_us = kTokenUs[tiles] * token_factor;
         for (int len = most; len >= kPairTokens; len = len * 3 / 4 / kPairTokens * kPairTokens) {
             double longest = 0.0, sum = 0.0, count = 0.0;
             for_each_job([&](int tokens, int64_t rows) {
@@ -189,15 +201,12 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double tick
                 const double blocks = (double)((rows + 16 * tiles - 1) / (16 * tiles)) * Hkv * chunks;
                 const double us = kBlockUs[tiles] + each * token_us, join_us = chunks > 1 ? ticket_us + chunks * kJoinUs[tiles] : 0.0;
                 longest = std::max(longest, us + join_us);
-                sum += blocks * us;
+                sum += blocks * (kBlockUs[tiles] + each * token_us * busy_tokens);
                 count += blocks;
             });
             const double busy = sum / (units * kSecondBlock), us = std::max(longest, count > units ? busy + 0.5 * longest : 0.0);
-            if (us < best_us * 0.97) {   // (fewer tiles or shorter chunks only for something)
-                best_us = us;
-                best = {tiles, len};
-            }
-            if (busy >= best_us) break;   // (shorter chunks are more work in all)
+            if (us < best.us * 0.97) best = {tiles, len, us};   // (fewer tiles or shorter chunks only for something)
+            if (busy >= best.us) break;   // (shorter chunks are more work in all)
         }
     }
     return best;
@@ -210,11 +219,11 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, bool full, double tick
 // partial results to write and to read back.
 constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kPieceJoinUs = 0.35;
 template <typename F>
-int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, F for_each_group)   // for_each_group(f): f(row blocks, steps)
+int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
 {
     const double units = compute_units(), factor = d / 128.0 * (full ? (codes ? 1.5 : 2.0) : 1.0);   // (more terms: more products with V)
     int best = std::min(most_steps, kMaxPrefixSteps);
-    double best_us = 1e30;
+    best_us = 1e30;
     for (int len = best; len >= 1; len = std::min(len - 1, len * 7 / 8)) {
         double count = 0.0, sum = 0.0, longest = 0.0, pieces = 0.0;
         for_each_group([&](int64_t row_blocks, int steps) {
@@ -243,6 +252,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
     memset(&pl, 0, sizeof pl);
     const int group = a->Hq / a->Hkv;
     const bool full = a->out_dtype == SPEC_F32;
+    const double token_factor = (full ? kFullFactor : 1.0) * (a->d == 64 ? kShortFactor : 1.0);
     int max_q = 0, max_own = 0, max_len = 0;
     auto prefix_of = [&](int &g, int b) {
         if (a->G == 0) return 0;
@@ -260,17 +270,15 @@ Plan make_plan(const spec_prefix_attn_args *a)
     const int max_rows = std::max(max_q * group, 1);
     pl.max_q_rows = max_rows;
     pl.capacity = a->max_kv_len > 0 ? a->max_kv_len : max_len;
-    const Split own = split_jobs(max_rows, max_own, a->Hkv, full, kTicketUs, [&](auto job) {
-        for (int b = 0, g = 0; b < a->B; ++b) {
-            const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = prefix_of(g, b);
-            if (q > 0) job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, q * group);
-        }
-    });
-    pl.row_tiles = own.tiles;
-    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
-    pl.chunk_tokens = own.length;
-    pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
-    pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
+    auto split_own = [&](int most_tokens, bool whole, double busy_tokens) {
+        return split_jobs(max_rows, most_tokens, a->Hkv, token_factor, kTicketUs, busy_tokens, [&](auto job) {
+            for (int b = 0, g = 0; b < a->B; ++b) {
+                const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = whole ? 0 : prefix_of(g, b);
+                if (q > 0) job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, q * group);
+            }
+        });
+    };
+    Split own = split_own(max_own, false, 1.0);
     int max_prefix = 0;
     int64_t most_rows = 0;
     for (int g = 0; g < a->G; ++g) {
@@ -279,6 +287,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
     }
     if (max_prefix > 0 && most_rows > 0) {
         pl.prefix_capacity = max_prefix;
+        double prefix_us = 0.0;
         pl.prefix_many_rows = most_rows > 16 * kMostTiles;
         auto rows_of = [&](int g) { return (int64_t)(a->host_cu_q_len[a->host_cu_group[g + 1]] - a->host_cu_q_len[a->host_cu_group[g]]) * group; };
         if (pl.prefix_many_rows) {
@@ -287,7 +296,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
             auto each_group = [&](auto group) {
                 for (int g = 0; g < a->G; ++g) group((rows_of(g) + kPrefixRows - 1) / kPrefixRows, steps_of(a->host_prefix_len[g]));
             };
-            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, each_group);
+            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, prefix_us, each_group);
             each_group([&](int64_t row_blocks, int steps) {
                 pl.prefix_blocks += row_blocks * ((steps + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps) * a->Hkv;
             });
@@ -295,10 +304,11 @@ Plan make_plan(const spec_prefix_attn_args *a)
             pl.prefix_row_blocks = (int)std::min<int64_t>(pl.prefix_blocks, INT32_MAX);
             pl.max_prefix_chunks = (steps_of(max_prefix) + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps;
         } else {
-            const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, full, 0.0, [&](auto job) {   // (no ticket: the next launch joins)
+            const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, token_factor, 0.0, 1.0, [&](auto job) {   // (no ticket: the next launch joins)
                 for (int g = 0; g < a->G; ++g)
                     if (a->host_prefix_len[g] > 0) job(a->host_prefix_len[g], rows_of(g));
             });
+            prefix_us = split.us;
             pl.prefix_tiles = split.tiles;
             pl.prefix_chunk_tokens = split.length;
             // (as many row blocks as the rows can make however they are spread over the groups)
@@ -306,7 +316,32 @@ Plan make_plan(const spec_prefix_attn_args *a)
             pl.max_prefix_chunks = (max_prefix + pl.prefix_chunk_tokens - 1) / pl.prefix_chunk_tokens;
             pl.prefix_blocks = (int64_t)pl.prefix_row_blocks * a->Hkv * pl.max_prefix_chunks;
         }
+        const double token_bytes = a->kv_dtype == SPEC_BF16 ? 4.0 * a->d : 2.0 * a->d + 8.0;   // of a KV head
+        double prefix_tokens = 0.0, walked_tokens = 0.0;   // of the prefixes; of what the requests walk of them
+        for (int g = 0; g < a->G; ++g) {
+            prefix_tokens += a->host_prefix_len[g];
+            for (int b = a->host_cu_group[g]; b < a->host_cu_group[g + 1]; ++b)
+                if (a->host_cu_q_len[b + 1] > a->host_cu_q_len[b]) walked_tokens += a->host_prefix_len[g];
+        }
+        const bool near = a->kv_dtype != SPEC_BF16 && prefix_tokens * token_bytes <= kNearBytes;
+        const Split whole = split_own(max_len, true, near ? kCachedTokens : kFarTokens);
+        const double more = a->kv_dtype == SPEC_BF16 ? kWholeBf16 : a->kv_dtype == SPEC_INT8 ? kWholeInt8 : 1.0;
+        const double whole_us = std::max(whole.us * more, walked_tokens * token_bytes * a->Hkv / kCacheBytesPerUs);
+        const double shared_us = std::max((own.us + prefix_us) * kTwoLaunches, prefix_tokens * token_bytes * a->Hkv / kMemoryBytesPerUs) + kLaunchUs;
+        const int shared = prefix_shared_switch();
+        if (shared < 0 ? whole_us < shared_us : shared == 0) {
+            own = whole;
+            max_own = max_len;
+            pl.whole_context = 1;
+            pl.max_prefix_chunks = 0;
+            pl.prefix_blocks = pl.prefix_row_blocks = 0;
+        }
     }
+    pl.row_tiles = own.tiles;
+    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
+    pl.chunk_tokens = own.length;
+    pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
+    pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
     const size_t rows = (size_t)a->T * a->Hq;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes); return here; };
@@ -342,10 +377,11 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     memset(&p, 0, sizeof p);
     p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.group = a->Hq / a->Hkv; p.num_blocks = a->num_blocks; p.max_blocks_per_req = a->max_blocks_per_req;
     p.T = a->T;
-    p.G = pl.max_prefix_chunks > 0 ? a->G : 0;   // (groups without a prefix are single requests)
+    p.G = pl.max_prefix_chunks > 0 || pl.whole_context ? a->G : 0;   // (groups without a prefix are single requests)
     p.kind = a->kv_dtype == SPEC_E4M3 ? kCacheE4M3 : a->kv_dtype == SPEC_INT8 ? kCacheInt8 : a->kv_layout == SPEC_KV_MFMA ? kCacheTiles : kCacheTokens;
     p.d = a->d;
     p.out_f32 = a->out_dtype == SPEC_F32;
+    p.whole_context = pl.whole_context;
     p.row_tiles = pl.row_tiles; p.row_blocks = pl.row_blocks; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks;
     p.capacity_tokens = pl.capacity; p.max_q_rows = pl.max_q_rows;
     p.prefix_tiles = pl.prefix_tiles; p.prefix_many_rows = pl.prefix_many_rows; p.prefix_piece_steps = pl.prefix_piece_steps; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;

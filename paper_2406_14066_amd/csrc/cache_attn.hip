@@ -88,6 +88,7 @@ struct Shared {
 // The block's place in the work.
 struct Work {
     int b;             // request whose block-table row says where the pages are
+    int head, head_pages;   // ... but for its first pages another one's
     int kvh, chunk, nchunks;
     int row0, rows;    // first packed token row, fused query rows from there on
     int row_lo;        // first of them that is this block's
@@ -217,19 +218,24 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
     const bool first = w.chunk == 0 && w.kvh == 0 && w.row_block == 0;
     int P = 0;
     w.group_index = 0;
+    w.head = w.b;
     if (p.G > kWave) {
         w.group_index = group_of(p, w.b);
         P = uniform_load(p.prefix_len, w.group_index);
+        w.head = uniform_load(p.cu_group, w.group_index);
     } else if (p.G > 0) {
         w.group_index = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < p.G && w.end_of_group <= w.b)), p.G - 1);
         P = __builtin_amdgcn_readlane(w.prefix_of_group, w.group_index);
+        w.head = __builtin_amdgcn_readlane(w.first_of_group, w.group_index);
     }
-    w.prefix = P;
+    const int own_from = p.whole_context ? 0 : P;
+    w.prefix = own_from;
+    w.head_pages = p.whole_context ? P / SPEC_BLOCK_SIZE : 0;
     // The lengths come from device memory and bound every loop and index below: a request whose lengths do not fit
     // the launch is left out and reported.
     if (q_len < 0 || q_len > SPEC_K_MAX + 1 || w.row0 < 0 || w.row0 + q_len > p.T || q_len * p.group > p.max_q_rows || L < 0 ||
         L > p.capacity_tokens || (L + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE > p.max_blocks_per_req || !prefix_ok(p, P) ||
-        (P > 0 && L - q_len < P)) {
+        (P > 0 && (L - q_len < P || w.head < 0 || w.head > w.b))) {
         count_error(p, first);
         return false;
     }
@@ -237,7 +243,7 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
     w.row_lo = w.row_block * (NT * 16);
     if (w.row_lo >= w.rows) return false;
     // even chunks per request, page aligned; a request without tokens has one that is empty
-    const int tokens = L - P;
+    const int tokens = L - own_from;
     w.nchunks = p.max_chunks == 1 ? 1 : max(min(chunk_count(tokens, p.chunk_tokens), p.max_chunks), 1);
     if (w.chunk >= w.nchunks) return false;
     const int C = w.nchunks == 1 ? tokens : ((tokens + w.nchunks - 1) / w.nchunks + SPEC_BLOCK_SIZE - 1) & ~(SPEC_BLOCK_SIZE - 1);
@@ -245,7 +251,7 @@ __device__ __forceinline__ bool place_own(const CacheAttnParams &p, Work &w)
         count_error(p, first);
         return false;
     }
-    w.tok0 = min(P + w.chunk * C, L);
+    w.tok0 = min(own_from + w.chunk * C, L);
     w.tok1 = min(w.tok0 + C, L);
     w.hide_from = L - q_len + 1;
     return true;
@@ -337,7 +343,7 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, Work &w)
     w.tok0 = min(w.chunk * C, P);
     w.tok1 = min(w.tok0 + C, P);
     w.hide_from = 0x7FFFFFFF - SPEC_K_MAX - 1;
-    w.prefix = 0;
+    w.prefix = w.head = w.head_pages = 0;
     return true;
 }
 
@@ -399,13 +405,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     bool some_bad;
     {
         const bool used = mine < npages;
-        if (used) bt = p.block_table[(size_t)w.b * p.max_blocks_per_req + w.tok0 / SPEC_BLOCK_SIZE + mine];
+        const int page = w.tok0 / SPEC_BLOCK_SIZE + mine;
+        if (used) bt = p.block_table[(size_t)(page < w.head_pages ? w.head : w.b) * p.max_blocks_per_req + page];
         const bool bad = used && (unsigned)bt >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
         if (bad) bt = -1;
         const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
         some_bad = bad_lanes != 0;
-        if (some_bad && w.kvh == 0 && w.row_block == 0 && lane == 0 && p.errors != nullptr)
-            atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
+        if (some_bad && w.kvh == 0 && w.row_block == 0 && p.errors != nullptr) {   // (a shared page: by the group's first rows)
+            const unsigned long long shared = __builtin_amdgcn_ballot_w64(bad && page < w.head_pages);
+            const int n = __builtin_popcountll(w.row0 == uniform_load(p.cu_q_len, w.head) ? bad_lanes : bad_lanes & ~shared);
+            if (lane == 0 && n > 0) atomicAdd(p.errors, (unsigned long long)n);
+        }
     }
     const int npairs = (npages + 1) / 2;
     const int my_pairs = npairs > wave ? (npairs - wave + kWaves - 1) / kWaves : 0;

@@ -59,6 +59,7 @@ struct CacheAttnParams {
     int32_t kind, d, out_f32;
     int32_t row_tiles, row_blocks;              // own: 16-row tiles of a block, blocks that cover a request's rows
     int32_t chunk_tokens, max_chunks;           // own tokens
+    int32_t whole_context;                      // own: of the prefix too, which no other launch takes then
     int32_t capacity_tokens;                    // longest kv_len planned for
     int32_t prefix_tiles, prefix_row_blocks;    // prefix: 16-row tiles of a block, blocks over all groups
     int32_t prefix_chunk_tokens, max_prefix_chunks;   // 0: no group has a prefix
@@ -79,5 +80,8 @@ struct CacheAttnParams {
     unsigned long long *errors;
 };
 hipError_t launch_cache_attn(const CacheAttnParams &p, hipStream_t stream);
+
+// The tuning switch SPEC_VERIFY_PREFIX_SHARED: 0 / 1, or -1: the planner's choice.
+int prefix_shared_switch();
 
 }  // namespace specv

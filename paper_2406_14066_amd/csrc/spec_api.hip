@@ -6,6 +6,7 @@
 // checks, the split of the KV length, the order table and the grid layout are computed when a
 // shape is seen for the first time), and the launch.  The tuning switches are read from the
 // environment once.
+#include "cache_ops.h"
 #include "common.h"
 
 #include <math.h>
@@ -107,6 +108,8 @@ struct Tuning {
     int k_direct = -1;            // SPEC_VERIFY_K_DIRECT=0/1: the attention alone on token-major pages, K through LDS or straight into
                                   // operand order where there is a kernel for it (-1: automatic)
     int f32_scalar = -1;          // SPEC_VERIFY_F32_SCALAR=0/1: fp32 attention alone on the matrix-instruction / scalar kernel (-1: automatic)
+    int prefix_shared = -1;       // SPEC_VERIFY_PREFIX_SHARED=0/1: requests behind a prefix walk their whole contexts / the prefix has a launch of its own
+                                  // (-1: automatic)
     int spin_limit = 1 << 20;     // SPEC_VERIFY_SPIN_LIMIT: polls of a bounded wait (about two seconds at the default)
     uint32_t epoch = 1;           // changes with every reload: part of the plan cache's key
 };
@@ -147,6 +150,7 @@ void read_tuning()
     if (const char *e = getenv("SPEC_VERIFY_REJECT_EVEN")) t.reject_even = e[0] != '0';
     if (const char *e = getenv("SPEC_VERIFY_K_DIRECT")) t.k_direct = e[0] != '0';
     if (const char *e = getenv("SPEC_VERIFY_F32_SCALAR")) t.f32_scalar = e[0] != '0';
+    if (const char *e = getenv("SPEC_VERIFY_PREFIX_SHARED")) t.prefix_shared = e[0] != '0';
     if (const char *e = getenv("SPEC_VERIFY_SPIN_LIMIT")) {
         const long v = strtol(e, nullptr, 10);
         if (v >= 1 && v <= (1 << 30)) t.spin_limit = (int)v;
@@ -1001,6 +1005,8 @@ spec_status step_on_workspace(const spec_attn_args *attn, const spec_reject_args
 }
 
 }  // namespace
+
+int prefix_shared_switch() { return tuning().prefix_shared; }
 
 }  // namespace specv
 
