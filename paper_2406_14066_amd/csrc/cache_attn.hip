@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;
     constexpr int KK = D / 32, MT = D / 16;
     constexpr int kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);   // of one KV head
-    constexpr int TERMS = FULL ? (B8 ? 2 : 3) : 1;   // 16-bit terms of a softmax weight: 22 bits of fp16's, 24 of bf16's
+    constexpr int TERMS = FULL ? (B8 ? 2 : 3) : (B8 ? 1 : 2);   // 16-bit terms of a softmax weight: 11 or 22 bits of fp16's, 16 or 24 of bf16's
     constexpr float kTop = B8 ? 7.0f : 0.0f;         // fp16 weights go up to 2^(7 + slack): their small ones stay normal numbers
     typedef std::conditional_t<B8, f16x8, bf16x8> Weights;
     __shared__ Shared<KIND, NT, D> sh;
