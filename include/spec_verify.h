@@ -421,7 +421,8 @@ spec_status spec_kv8_attn(const spec_kv8_attn_args *args, void *workspace, size_
 /*
  * Lookahead attention of a batch that comes in groups: the requests cu_group[g] .. cu_group[g+1]-1 have their first
  * prefix_len[g] tokens (whole pages) in common, and the block-table row of the group's first request says where they
- * are.  Those tokens are read and multiplied once for all query rows of the group; the tokens after them are each request's own.
+ * are.  Where that is less work, those tokens are read and multiplied once for all query rows of the group, by a launch of their own;
+ * otherwise every request walks them with its own tokens, mostly from the caches.  The tokens after them are each request's own.
  * The result is spec_verify_attn's (bf16 pools) or spec_kv8_attn's (8-bit pools).  A group of one request or a
  * prefix of 0 tokens is an ordinary request.  Every query row sees its group's whole prefix: requests with rows have
  * kv_len[b] - q_len[b] >= prefix_len[g].
@@ -431,7 +432,8 @@ typedef struct {
     int32_t G;                    /* groups, G >= 1 */
     int32_t kv_dtype;             /* SPEC_BF16, SPEC_E4M3 or SPEC_INT8 */
     int32_t kv_layout;            /* SPEC_BF16: spec_kv_layout; 8-bit pools: SPEC_KV_MFMA */
-    int32_t out_dtype;            /* SPEC_F32: softmax weights as two (bf16 pools: three) 16-bit terms; SPEC_BF16: as one */
+    int32_t out_dtype;            /* SPEC_F32: softmax weights as two (bf16 pools: three) 16-bit terms; SPEC_BF16: as one (bf16 pools: two,
+                                     but one in the launch for prefixes with more than 48 query rows, whose results are fp16) */
     int32_t max_kv_len;           /* length bucket, as in spec_attn_args: the lengths in kv_len may change under a captured
                                      launch; the groups and their prefixes are part of the plan */
     int64_t q_token_stride;       /* as in spec_kv8_attn_args */

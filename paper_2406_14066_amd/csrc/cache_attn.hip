@@ -23,11 +23,11 @@
 
 namespace specv {
 
-// Variants are chosen by (row tiles, head dim, weights in more than one term); one set per kind of cache.
+// Variants are chosen by (row tiles, head dim, type of the output); one set per kind of cache.
 struct CacheLaunch {
     dim3 blocks;
     int prefix;      // which of the two launches
-    int many_rows;   // the prefix's blocks take 4 * tiles row tiles each
+    int many_rows;   // the prefix's is prefix_rows_kernel's
 };
 template <int KIND>
 hipError_t launch_cache_kind(const CacheAttnParams &p, int tiles, bool full, CacheLaunch at, hipStream_t stream);
@@ -370,6 +370,19 @@ struct RowSum {
     }
 };
 
+// ---------------------------------------------------------------------------
+// One block: a row block of NT 16-row tiles through a chunk of a request's tokens (or, prefix = 1, of a group's prefix, with at most 48 query
+// rows behind it).  Four wavefronts take the chunk's pairs of pages in turn and never wait for each other before the end: K and V go
+// from memory into a wavefront's registers in operand order, and each part of them asks for the next pair as soon as it has been used.
+//
+// What bounds it: with many blocks the bytes of the cache (256 requests of 256 .. 1024 tokens on 64/8 heads, 8-bit, k = 2: 371 MB in
+// 71 us, 5.2 TB/s); with wide rows the instructions of a step, which are conversions and softmax more than matrix products (4 requests of
+// 6000 .. 32768 tokens, int8, 36 rows, fp32 output: 58 us, 3.8 TB/s; counters: vector instructions 53% of the wavefronts' cycles, matrix
+// instructions 27%, waits 23%); with few blocks latency (one request of 687 tokens: 6.9 us, of which 3.8 is an empty launch).
+// Hence one wavefront a SIMD with as many registers as that allows, the queries in LDS (NT > 1), descriptors and scales by a
+// few instructions, masks only in the steps that need them.  Eight wavefronts a block, a block order that keeps a request on an XCD, and
+// three blocks on a compute unit (registers spilled) were all slower.
+// ---------------------------------------------------------------------------
 template <int KIND, int NT, int D, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams p, int prefix)
 {
@@ -386,8 +399,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, g = lane >> 4;
     const int rows = min(w.rows - w.row_lo, NT * 16);   // this block's
 
-    // Q goes to LDS and comes back as the B operand of S^T = K Q^T when it is needed, which keeps registers for pages on
-    // their way: lane (g, n) takes row n, the 8 dims that the lane's K holds (bf16 pages: 32 kk + 8 g ..; 8-bit pages, 16
+    // Q goes to LDS and comes back as the B operand of S^T = K Q^T when it is needed (a single tile: once, for good), which keeps
+    // registers for pages on their way: lane (g, n) takes row n, the 8 dims that the lane's K holds (bf16 pages: 32 kk + 8 g ..; 8-bit pages, 16
     // bytes of which are two operands: 64 (kk / 2) + 16 g + 8 (kk % 2) ..)
     constexpr int QP = D / 8, QN = (NT * 16 * QP + kThreads - 1) / kThreads;   // 16-byte pieces of a row, of a thread
     u32x4 q_piece[QN];
@@ -921,7 +934,16 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 //   S^T[token][row] = K[token][:] . Q[row][:]: a pair, 16 dims per instruction, lane (half, c) holds row c, tokens
 //   4 half + 8 i + 0..3, i = 0, 1 of the first page, 2, 3 of the second
 //   O^T[dim][row] += V^T[dim][token] . P^T[token][row]: a page per instruction, its tokens in that order
-// Two LDS buffers and one barrier per step.
+// Two LDS buffers and one barrier per step; operands are read four reads ahead of the products that take them, and both pairs'
+// scores come before one look at the running maximum, so that the second pair's weights are made under the first one's products.
+//
+// What bounds it: behind one prefix of 4096 tokens, 64 requests, 64/8 heads, k = 2, bf16, the launch takes 37 us.  Two blocks on a compute
+// unit walk a step each in 1.87 us, 1.15 PFLOP/s over the device (a product of two 8192 x 8192 bf16 matrices reaches 1.31, of 4096 x 4096
+// 1.10), for 24 of them; the rest is the start (finding the group, the table, the first pages: 5), the partial results (2.5) and the
+// launch.  8-bit pages add the conversions and the scales (three prefixes of 6000 .. 20000 tokens, 40 rows a request: 133 us,
+// 0.64 PFLOP/s).  64 rows a wavefront would halve the operand reads, but its accumulators go to the second register file and come back
+// for every use of the others (37 -> 54 us); three blocks on a compute unit with one pair a step do as well but leave half as many
+// partial results again.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int KIND, int D>

@@ -39,13 +39,13 @@ struct Kv8ReadParams {
 };
 hipError_t launch_kv8_read(const Kv8ReadParams &p, hipStream_t stream);
 
-// Attention over a paged cache in up to two launches.
+// Attention over a paged cache in one launch or two.
 //   prefix   one block per (row block of a group, KV head, chunk of the group's prefix): partial results of all the group's
-//            query rows, which see the whole prefix.
-//   own      one block per (request, row block, KV head, chunk of the tokens after the prefix): the tokens that are the
-//            request's alone, causal inside the draft.  A request whose own tokens are one chunk takes its prefix
-//            partials in and writes the output; otherwise the last of its blocks to finish merges all partials (tickets).
-// Partial results of query row r (token row * Hq + head), chunk c:
+//            query rows, which see the whole prefix.  Groups with more than 48 rows have a kernel of their own (many rows).
+//   own      one block per (request, row block, KV head, chunk of the tokens after the prefix, or of all tokens where there is no
+//            prefix launch), causal inside the draft.  A request whose tokens are one chunk takes its prefix partials in and
+//            writes the output; otherwise the last of its blocks to finish joins its partials first (tickets).
+// Partial results of query row r (token row * Hq + head), chunk (or piece) c:
 //   acc [r][max chunks][d]  sum_t 2^(x_t - m) V_t, un-normalised    ml [r][max chunks][2]  m and sum_t 2^(x_t - m)
 // in fp32 (prefixes with many rows and a bf16 output: acc in fp16).
 constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's four wavefronts: 64 pages each

