@@ -992,11 +992,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
     const int kvh = block / total;
     if (kvh >= p.Hkv) return;
     rest -= kvh * total;
-    for (int base = kWave; rest >= all; base += kWave) {   // (more than 64 groups; rest < total)
+    for (int base = kWave; rest >= all && base < p.G; base += kWave) {   // (more than 64 groups)
         rest -= all;
         work.look(p, base + lane);
         upto = running_sum(work.blocks, all);
     }
+    if (rest >= all) return;
     {
         const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > rest));
         rest -= __builtin_amdgcn_readlane(upto - work.blocks, who);

@@ -87,11 +87,17 @@ __device__ __forceinline__ int request_of(const int32_t *cu, int B, int row, int
 // enough for n = cu[b+1] - cu[b] tokens from any position: those touch at most n / 16 + 2 pages.
 __host__ __device__ __forceinline__ int page_item(int packed, int b) { return packed / SPEC_BLOCK_SIZE + 2 * b; }
 
-// The request that owns an item: the last one whose first item is not beyond it.  A wavefront asks 64 places at a time (256 requests:
-// two loads one after another, where halving takes eight).
-__device__ __forceinline__ int request_of_item(const int32_t *cu, int B, int item)
+// The request that owns an item: the last one whose first item is not beyond it.  A wavefront asks 64 places at a time: those about
+// the place where it is if all requests are alike, then all of them at even distances (256 requests: two more loads one after
+// another, where halving takes eight).
+__device__ __forceinline__ int request_of_item(const int32_t *cu, int B, int item, int items)
 {
     const int lane = threadIdx.x % kWave;
+    if (B > kWave) {
+        const int base = min(max((int)((int64_t)item * B / items) - kWave / 2, 0), B - kWave), at = base + lane;
+        const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(page_item(cu[at], at) <= item));
+        if (count > 0 && (count < kWave || base == B - kWave)) return base + count - 1;
+    }
     int lo = 0, n = B;
     while (n > 1) {
         const int stride = (n + kWave - 1) / kWave, at = lo + lane * stride;

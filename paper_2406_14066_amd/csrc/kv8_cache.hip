@@ -37,15 +37,17 @@ __device__ __forceinline__ bool place_page(PageWork &w, int pos0, int n, int row
 
 // Append: a wavefront per (page that a request's rows touch, KV head).  Lane (s, g) = (lane % 16, lane / 16) takes token slot s,
 // dims g D/4 .. + D/4 - 1: a token's maximum is one exchange between four lanes.  K's codes are 16-byte pieces of the page
-// as they are; V's, four tokens to a word, are transposed between the lanes of a quad, and go out as words where all four
-// tokens are new and as bytes where some are not (their old neighbours stay untouched without being read).
-// Rows of long prompts are bound by the bytes (16000 tokens, 8 heads, d = 128, bf16 rows inside a fused projection: 64 MB in 16 us,
-// 4.0 TB/s), a step's five rows of 256 requests by the chain lengths -> table -> rows -> stores and the partly written lines
-// (9.3 us; an empty launch takes 3.8, one row of one request 5).
+// as they are; V's, four tokens to a word, are transposed between the lanes of a quad and gathered through LDS into the page's
+// 16-byte cells (4 tokens of 4 dims), which go out whole where all four tokens are new and by halves and bytes of words where some
+// are not (their old neighbours stay untouched without being read).
+// Rows of long prompts are bound by the bytes (16000 tokens, 8 heads, d = 128, bf16 rows inside a fused projection: 64 MB in 13.7 us,
+// 4.7 TB/s; 16.0 with V's words stored one by one), a step's five rows of 256 requests by the chain lengths -> table -> rows -> stores and the partly written lines
+// (8.4 us; an empty launch takes 3.8, one row of one request 5).
 template <typename T, bool INT8, int D>
 __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8AppendParams p, int items)
 {
     constexpr int N = D / 4;        // dims per lane
+    __shared__ alignas(16) unsigned char stage[kPageWaves][SPEC_BLOCK_SIZE * D];
     constexpr float kMost = INT8 ? kMaxInt8 : kMaxE4M3;
     const int lane = threadIdx.x % kWave, s = lane & 15, g = lane >> 4;
     const int unit = (int)(blockIdx.x * kPageWaves + threadIdx.x / kWave);
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
     if (item >= items) return;   // (the wavefronts of a block are independent)
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
-    w.b = request_of_item(p.cu_q_len, p.B, item);
+    w.b = request_of_item(p.cu_q_len, p.B, item, items);
     const int row0 = p.cu_q_len[w.b], n = p.cu_q_len[w.b + 1] - row0;
     if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
     const int pos0 = p.kv_len[w.b] - n;
@@ -111,21 +113,35 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
             }
         } else {
             // after the transposition lane (s, g) holds, per j, dim g N + 4 j + s % 4 of the tokens s & ~3 .. + 3
-            unsigned char *page = p.v_cache + head * (SPEC_BLOCK_SIZE * D);
-            const int a4 = s & 3, t0 = s & ~3;
-#pragma unroll
-            for (int j = 0; j < N / 4; ++j) code[j] = transpose_quad(code[j], a4);
-            const bool whole = t0 >= w.s0 && t0 + 4 <= w.s1;
+            unsigned char *page = p.v_cache + head * (SPEC_BLOCK_SIZE * D), *st = stage[threadIdx.x / kWave];
+            const int a4 = s & 3;
 #pragma unroll
             for (int j = 0; j < N / 4; ++j) {
                 const int dim = g * N + 4 * j + a4;
-                unsigned char *at = page + ((dim / 64 * 4 + t0 / 4) * 16 + dim % 16) * 16 + dim % 64 / 16 * 4;
-                if (whole) {
-                    *reinterpret_cast<uint32_t *>(at) = code[j];
-                } else {
+                *reinterpret_cast<uint32_t *>(st + ((dim / 64 * 4 + (s >> 2)) * 16 + dim % 16) * 16 + dim % 64 / 16 * 4) = transpose_quad(code[j], a4);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            // lane (n, g) takes the cells of tokens 4 g .. + 3: those from t0 up to t1 are new
+            const int t0 = min(max(w.s0 - 4 * g, 0), 4), t1 = min(max(w.s1 - 4 * g, 0), 4);
+            const bool whole = t0 == 0 && t1 == 4, low = t0 == 0 && t1 >= 2, high = t0 <= 2 && t1 == 4;   // both tokens of a half
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (t0 + t >= w.s0 && t0 + t < w.s1) at[t] = (unsigned char)(code[j] >> (8 * t));
+            for (int i = 0; i < D / 64; ++i) {
+                const u32x4 cell = *reinterpret_cast<const u32x4 *>(st + i * 1024 + lane * 16);
+                unsigned char *at = page + i * 1024 + lane * 16;
+                if (whole) {
+                    *reinterpret_cast<u32x4 *>(at) = cell;
+                } else if (t0 < t1) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (low) *reinterpret_cast<uint16_t *>(at + 4 * e) = (uint16_t)cell[e];
+                        else if (t0 == 0) at[4 * e] = (unsigned char)cell[e];
+                        else if (t0 == 1) at[4 * e + 1] = (unsigned char)(cell[e] >> 8);
+                        if (high) *reinterpret_cast<uint16_t *>(at + 4 * e + 2) = (uint16_t)(cell[e] >> 16);
+                        else if (t0 <= 2 && t1 == 3) at[4 * e + 2] = (unsigned char)(cell[e] >> 16);
+                        else if (t0 == 3) at[4 * e + 3] = (unsigned char)(cell[e] >> 24);
+                    }
                 }
             }
         }
@@ -147,7 +163,7 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_read_kernel(Kv8ReadPara
     if (item >= items) return;   // (the wavefronts of a block are independent)
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
-    w.b = request_of_item(p.cu_len, p.B, item);
+    w.b = request_of_item(p.cu_len, p.B, item, items);
     const int row0 = p.cu_len[w.b], n = p.cu_len[w.b + 1] - row0;
     if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
     const int pos0 = p.start != nullptr ? p.start[w.b] : 0;

@@ -137,3 +137,36 @@ def test_a_table_entry_outside_the_pool_reads_as_zeros_anywhere():
         want, most = _want(plain, q, bad_whole, kv_len, cu)
         assert errors == 2
         check(got, want, "f32", most)
+
+
+@pytest.mark.parametrize("counts", ["alike", "ragged", "one_long", "mostly_empty"])
+def test_append_finds_every_request_of_a_large_batch(counts):
+    """More requests than lanes of a wavefront, alike and not: every row goes where its request's table says, and comes back."""
+    import torch
+    rng = np.random.default_rng(9)
+    B, Hkv, d = 333, 2, 64
+    n = {"alike": np.full(B, 5), "ragged": rng.integers(0, 40, B), "one_long": np.where(np.arange(B) == 200, 3000, 1),
+         "mostly_empty": np.where(rng.random(B) < 0.03, 17, 0)}[counts]
+    before = rng.integers(0, 50, B)
+    kv_len = (before + n).astype(np.int32)
+    cu = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    pages = (kv_len + 15) // 16
+    nb = int(pages.sum()) + 1
+    order = rng.permutation(nb)[:int(pages.sum())]
+    table = np.zeros((B, int(pages.max())), dtype=np.int32)
+    at = 0
+    for b in range(B):
+        table[b, :pages[b]] = order[at:at + pages[b]]
+        at += pages[b]
+    rows = torch.randint(-127, 128, (int(cu[-1]), 2 * Hkv, d), device="cuda").float()
+    rows[:, :, 0] = 127.0        # scale 1: every value comes back as it is
+    k, v, scale = sv.alloc_kv8_pools(nb, Hkv, d, torch.int8)
+    dev = [torch.from_numpy(x).cuda() for x in (table, kv_len, cu, before.astype(np.int32))]
+    errors = torch.zeros(1, dtype=torch.int64, device="cuda")
+    args, keep = sv.make_kv8_append_args(rows[:, :Hkv], rows[:, Hkv:], k, v, scale, dev[0], dev[1], dev[2], kv_len, cu, error_count=errors)
+    sv.spec_kv8_append(args)
+    out = [torch.zeros((int(cu[-1]), Hkv, d), device="cuda") for _ in range(2)]
+    args, keep2 = sv.make_kv8_read_args(out[0], out[1], k, v, scale, dev[0], dev[3], dev[2], cu, error_count=errors)
+    sv.spec_kv8_read(args)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], rows[:, :Hkv]) and torch.equal(out[1], rows[:, Hkv:]) and int(errors.item()) == 0
