@@ -95,8 +95,9 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
         }
         const bool finite = most < 0x7F800000u;
         const float a = fmaxf(__uint_as_float(most), kSmallestRow);
-        scale[kv] = finite ? a / kMost : __uint_as_float(0x7FC00000u);
-        const float inv = kMost / a;
+        // (the two quotients as products with rounded reciprocals, as fp32 tensor arithmetic does them: codes at a tie agree with it)
+        scale[kv] = finite ? a * (1.0f / kMost) : __uint_as_float(0x7FC00000u);
+        const float inv = kMost * (1.0f / a);
         uint32_t code[N / 4];
 #pragma unroll
         for (int j = 0; j < N / 4; ++j) {

@@ -37,7 +37,7 @@ def quantise(row, kv):
     a = np.maximum(np.abs(row).max(-1), np.float32(2.0 ** -60)).astype(np.float32)
     most = np.float32(MOST[kv])
     with np.errstate(invalid="ignore", over="ignore"):
-        x = row * (most / a)[..., None]
+        x = row * ((np.float32(1) / a) * most)[..., None]
     bad = ~np.isfinite(row).all(-1)
     if kv == "int8":
         code = np.clip(np.rint(np.where(bad[..., None], 0, x)), -127, 127).astype(np.int8).view(np.uint8)
@@ -49,7 +49,7 @@ def quantise(row, kv):
         code = np.searchsorted(table, np.abs(v)).astype(np.uint8)
         assert (table[code] == np.abs(v)).all()
         code = np.where(np.signbit(x), code | 128, code).astype(np.uint8)
-    scale = np.where(bad, np.float32(np.nan), (a / most).astype(np.float32))
+    scale = np.where(bad, np.float32(np.nan), (a * (np.float32(1) / most)).astype(np.float32))
     return code, scale
 
 

@@ -170,3 +170,26 @@ def test_append_finds_every_request_of_a_large_batch(counts):
     sv.spec_kv8_read(args)
     torch.cuda.synchronize()
     assert torch.equal(out[0], rows[:, :Hkv]) and torch.equal(out[1], rows[:, Hkv:]) and int(errors.item()) == 0
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
+def test_codes_and_scales_are_those_of_fp32_tensor_arithmetic(kv):
+    """Bit for bit, ties included: M / a and a / M are products with rounded reciprocals in both."""
+    import torch
+    T, Hkv, d = 16 * 512, 8, 128
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    x = torch.randn((T, Hkv, d), generator=gen, device="cuda")
+    k, v, scale = sv.alloc_kv8_pools(T // 16, Hkv, d, torch.int8 if kv == "int8" else torch.float8_e4m3fn)
+    table = torch.arange(T // 16, dtype=torch.int32, device="cuda")[None]
+    cu = np.array([0, T], dtype=np.int32)
+    cud = torch.from_numpy(cu).cuda()
+    args, keep = sv.make_kv8_append_args(x, -x, k, v, scale, table, cud[1:], cud, cu[1:], cu)
+    sv.spec_kv8_append(args)
+    most = float(R.MOST[kv])
+    a = x.abs().amax(-1)
+    code = x * (most / a)[..., None]
+    code = torch.round(code).to(torch.int8) if kv == "int8" else code.clamp(-most, most).to(torch.float8_e4m3fn).view(torch.int8)
+    got = k.view(torch.int8).view(T // 16, Hkv, d // 16, 16, 16).permute(0, 3, 1, 2, 4).reshape(T, Hkv, d)
+    assert torch.equal(got, code)
+    assert torch.equal(scale[:, :, 0].permute(0, 2, 1).reshape(T, Hkv), a / most)
