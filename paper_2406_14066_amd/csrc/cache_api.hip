@@ -151,7 +151,7 @@ constexpr int kMostTiles = 3;   // row tiles of a block
 
 struct Plan {
     int whole_context, row_tiles, row_blocks, chunk_tokens, max_chunks, capacity, max_q_rows;
-    int prefix_tiles, prefix_many_rows, prefix_piece_steps, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
+    int prefix_tiles, prefix_many_rows, prefix_piece_steps, prefix_rows_log2, prefix_row_blocks, prefix_chunk_tokens, max_prefix_chunks, prefix_capacity;
     size_t acc, ml, tickets, prefix_acc, prefix_ml, total;   // offsets into the workspace
     int64_t blocks, prefix_blocks;
 };
@@ -215,13 +215,13 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, d
 // Most steps of a piece of the launch for prefixes with many rows, from a model of it.  A block takes kPieceUs besides its steps; a step
 // takes kStepUs while the block has its compute unit for itself, and kSharedStepUs where two share one, which is what fits: matrix cores and
 // vector units are busy at the same time more often (d = 128, weights in one term; measured behind one prefix of 4096 tokens, 64
-// requests, 64/8 heads, k = 2: 24 steps alone 32 us, 12 and 12 together 22 us).  More blocks than that take turns.  Each piece of a prefix is
+// requests, 64/8 heads, k = 2: 24 steps alone 32 us, 12 and 12 together 22 us; wide: a block of eight wavefronts has the unit, 13 steps 22 us).  More blocks than that take turns.  Each piece of a prefix is
 // partial results to write and to read back.
-constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kPieceJoinUs = 0.35;
+constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kWideStepUs = 1.7, kPieceJoinUs = 0.35;
 template <typename F>
-int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
+int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, bool wide, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
 {
-    const double units = compute_units(), factor = d / 128.0 * (full ? (codes ? 1.5 : 2.0) : 1.0);   // (more terms: more products with V)
+    const double units = compute_units(), slots = wide ? units : 2 * units, busy_us = wide ? kWideStepUs : kSharedStepUs, factor = d / 128.0 * (full ? (codes ? 1.5 : 2.0) : 1.0);   // (more terms: more products with V)
     int best = std::min(most_steps, kMaxPrefixSteps);
     best_us = 1e30;
     for (int len = best; len >= 1; len = std::min(len - 1, len * 7 / 8)) {
@@ -230,18 +230,18 @@ int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, do
             if (steps == 0) return;
             const int n = (steps + len - 1) / len, each = (steps + n - 1) / n;
             count += (double)row_blocks * n * Hkv;
-            sum += (double)row_blocks * n * Hkv * (kPieceUs + each * kSharedStepUs * factor);
+            sum += (double)row_blocks * n * Hkv * (kPieceUs + each * busy_us * factor);
             longest = std::max(longest, (double)each);
             pieces = std::max(pieces, (double)n);
         });
-        double us = kPieceUs + longest * factor * (count <= units ? kStepUs : kSharedStepUs);
-        if (count > 2 * units) us = std::max(us, sum / (2 * units) + 0.5 * longest * factor * kSharedStepUs);
+        double us = kPieceUs + longest * factor * (count <= units && !wide ? kStepUs : busy_us);
+        if (count > slots) us = std::max(us, sum / slots + 0.5 * longest * factor * busy_us);
         us += pieces * kPieceJoinUs;
         if (us < best_us) {
             best_us = us;
             best = len;
         }
-        if (sum / (2 * units) > best_us) break;   // (shorter pieces are more work in all)
+        if (sum / slots > best_us) break;   // (shorter pieces are more work in all)
     }
     return best;
 }
@@ -294,9 +294,19 @@ Plan make_plan(const spec_prefix_attn_args *a)
             constexpr int kStepTokens = kStepPages * SPEC_BLOCK_SIZE;
             auto steps_of = [&](int tokens) { return (tokens + kStepTokens - 1) / kStepTokens; };
             auto each_group = [&](auto group) {
-                for (int g = 0; g < a->G; ++g) group((rows_of(g) + kPrefixRows - 1) / kPrefixRows, steps_of(a->host_prefix_len[g]));
+                for (int g = 0; g < a->G; ++g) group((rows_of(g) + (1 << pl.prefix_rows_log2) - 1) >> pl.prefix_rows_log2, steps_of(a->host_prefix_len[g]));
             };
-            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, prefix_us, each_group);
+            // Blocks of eight wavefronts and 256 rows where that does not walk many more absent rows: pages are brought in and converted
+            // half as often (64 requests behind 4096 tokens, 64/8 heads, k = 2, bf16: 38.3 -> 34.4 us; three documents of 6000 ..
+            // 20000 tokens, e4m3: 142 -> 137).  With d = 64 more, smaller blocks are as good (15.7 us against 18.4, 18.0 against 16.5 in the next launch).
+            double padded[2] = {0.0, 0.0};
+            for (int wide = 0; wide < 2; ++wide) {
+                pl.prefix_rows_log2 = 7 + wide;
+                each_group([&](int64_t row_blocks, int steps) { padded[wide] += (double)(row_blocks << pl.prefix_rows_log2) * steps; });
+            }
+            const bool wide = a->d == 128 && padded[1] <= 1.1 * padded[0];
+            pl.prefix_rows_log2 = wide ? 8 : 7;
+            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, pl.prefix_rows_log2 == 8, prefix_us, each_group);
             each_group([&](int64_t row_blocks, int steps) {
                 pl.prefix_blocks += row_blocks * ((steps + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps) * a->Hkv;
             });
@@ -385,6 +395,7 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     p.row_tiles = pl.row_tiles; p.row_blocks = pl.row_blocks; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks;
     p.capacity_tokens = pl.capacity; p.max_q_rows = pl.max_q_rows;
     p.prefix_tiles = pl.prefix_tiles; p.prefix_many_rows = pl.prefix_many_rows; p.prefix_piece_steps = pl.prefix_piece_steps; p.prefix_row_blocks = pl.prefix_row_blocks; p.prefix_chunk_tokens = pl.prefix_chunk_tokens;
+    p.prefix_rows_log2 = pl.prefix_rows_log2;
     p.max_prefix_chunks = pl.max_prefix_chunks; p.prefix_capacity = pl.prefix_capacity;
     p.generation = next_generation();
     p.group_inverse = (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group);   // (unused where the group is 1)

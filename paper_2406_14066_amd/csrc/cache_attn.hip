@@ -159,7 +159,7 @@ struct GroupWork {
         pages = P / SPEC_BLOCK_SIZE;
         const int steps = (pages + kStepPages - 1) / kStepPages;
         pieces = (steps + p.prefix_piece_steps - 1) / p.prefix_piece_steps;
-        blocks = (rows + kPrefixRows - 1) / kPrefixRows * pieces;
+        blocks = ((rows + (1 << p.prefix_rows_log2) - 1) >> p.prefix_rows_log2) * pieces;
     }
     __device__ __forceinline__ void look(const CacheAttnParams &p, int g)
     {
@@ -923,12 +923,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 // ---------------------------------------------------------------------------
 // Prefixes of groups with many query rows.
 //
-// A block takes a row block of 128 rows through a piece of its group's prefix, counted in steps of four pages: the pieces of a prefix are
+// A block takes a row block of 128 or 256 rows through a piece of its group's prefix, counted in steps of four pages: the pieces of a prefix are
 // as even as they can be, and at most so long that the blocks of all groups fill the device (the host's choice).  Blocks lie KV head by KV
 // head, group by group, row block by row block, and consecutive ones on one XCD, which share their KV head's pages in its L2.
 //
-// A block's four wavefronts have 32 rows each and walk the same pages, which pass through LDS once for all of them, a step
-// (64 tokens, a page brought in by each wavefront) at a time.  In LDS the pages lie as the operands of v_mfma_f32_32x32x16 want
+// A block's wavefronts, four or eight, have 32 rows each and walk the same pages, which pass through LDS once for all of them, a step
+// (64 tokens, a page brought in by each wavefront or by two) at a time.  In LDS the pages lie as the operands of v_mfma_f32_32x32x16 want
 // them, 16 bytes per lane and 1 KB per read, as 16-bit values whatever the cache holds (8-bit codes are converted once on the
 // way in); token-major V is stored by rows and read through the transposing read.  (lane = 32 half + c; pair: two of the pages)
 //   S^T[token][row] = K[token][:] . Q[row][:]: a pair, 16 dims per instruction, lane (half, c) holds row c, tokens
@@ -937,16 +937,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 // Two LDS buffers and one barrier per step; operands are read four reads ahead of the products that take them, and both pairs'
 // scores come before one look at the running maximum, so that the second pair's weights are made under the first one's products.
 //
-// What bounds it: behind one prefix of 4096 tokens, 64 requests, 64/8 heads, k = 2, bf16, the launch takes 37 us.  Two blocks on a compute
-// unit walk a step each in 1.87 us, 1.15 PFLOP/s over the device (a product of two 8192 x 8192 bf16 matrices reaches 1.31, of 4096 x 4096
-// 1.10), for 24 of them; the rest is the start (finding the group, the table, the first pages: 5), the partial results (2.5) and the
-// launch.  8-bit pages add the conversions and the scales (three prefixes of 6000 .. 20000 tokens, 40 rows a request: 133 us,
-// 0.64 PFLOP/s).  64 rows a wavefront would halve the operand reads, but its accumulators go to the second register file and come back
-// for every use of the others (37 -> 54 us); three blocks on a compute unit with one pair a step do as well but leave half as many
-// partial results again.
+// What bounds it: behind one prefix of 4096 tokens, 64 requests, 64/8 heads, k = 2, bf16, the launch takes 34 us.  A block of eight
+// wavefronts on each compute unit walks a step in 1.7 us, 1.26 PFLOP/s over the device (a product of two 8192 x 8192 bf16 matrices reaches
+// 1.31, of 4096 x 4096 1.10), for 22 of them; the rest is the start (finding the group, the table, the first pages: 5), the partial
+// results (2.5) and the launch.  8-bit pages add the conversions and the scales (three prefixes of 6000 .. 20000 tokens, 40 rows a
+// request: 135 us, 0.63 PFLOP/s).  Two blocks of four wavefronts a unit take 38 and 142: they bring in and convert every page twice as
+// often.  64 rows a wavefront would halve the operand reads, but its accumulators go to the second register file and come back for
+// every use of the others (37 -> 54 us); three blocks of four wavefronts with one pair a step do as well as two of these but leave half as
+// many partial results again.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-template <int KIND, int D>
+template <int KIND, int D, int W>
 struct RowsShared {
     static constexpr int kK = kStepPages * SPEC_BLOCK_SIZE * D * 2;   // of a step
     static constexpr int kV = kStepPages * SPEC_BLOCK_SIZE * (KIND == kCacheTokens ? v_row_bytes(D) : D * 2);
@@ -956,17 +957,18 @@ struct RowsShared {
             alignas(16) unsigned char k[2][kK];   // [pair][16 dims][lane][16]
             alignas(16) unsigned char v[2][kV];   // [page][32-dim slice][lane][tokens 4 half .. + 3, 8 + 4 half .. + 3]; token-major: [page][token] rows
         };
-        alignas(16) unsigned char o[kWaves][32 * kOutRow];   // results on their way out, by half rows
+        alignas(16) unsigned char o[W][kPrefixRows * kOutRow];   // results on their way out, by half rows
     };
     // 8-bit pages, per token: K's scale with the softmax scale, log2 of V's, its reciprocal
     float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? kStepPages * SPEC_BLOCK_SIZE : 1];
     int page[kStepPages * (kMaxPrefixSteps + 4)];   // the steps' block-table entries, and four more steps'; -1: outside the pool, or past the end
-    static_assert(kStepPages * kMaxPrefixSteps == kThreads, "a thread per page");
+    static_assert(kStepPages * kMaxPrefixSteps <= W * kWave, "a thread per page");
 };
 
-template <int KIND, int D, bool FULL>
-__global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParams p)
+template <int KIND, int D, bool FULL, int W>
+__global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnParams p)
 {
+    constexpr int kPerPage = W / kStepPages;             // wavefronts that bring in a page
     constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;
     constexpr int KS = D / 16, SL = D / 32;
     constexpr int kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);
@@ -974,7 +976,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
     constexpr int TERMS = FULL ? (B8 ? 2 : 3) : 1;
     constexpr float kTop = B8 ? 7.0f : 0.0f;
     typedef std::conditional_t<B8, f16x8, bf16x8> Weights;
-    typedef RowsShared<KIND, D> Sh;
+    typedef RowsShared<KIND, D, W> Sh;
     __shared__ Sh sh;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1015,7 +1017,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
         steps = min(all_steps - first, each);
     }
     const int row0 = work.row0;                                 // the group's first packed token row
-    const int row_lo = row_block * kPrefixRows + wave * 32;
+    const int row_lo = (row_block * W + wave) * kPrefixRows;
     const int rows = min(max(work.rows - row_lo, 0), 32);       // this wavefront's
     auto out_index = [&](int r) {
         return packed_row(p, row0, kvh, row_lo + r);
@@ -1033,20 +1035,23 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
         }
         {
             const bool bad = used && (unsigned)entry >= (unsigned)p.num_blocks;   // never turned into an address: reads as zeros
-            sh.page[tid] = bad ? -1 : entry;
-            if (tid < 4 * kStepPages) sh.page[kThreads + tid] = -1;
+            if (tid < kStepPages * (kMaxPrefixSteps + 4)) sh.page[tid] = bad ? -1 : entry;
+            if (W * kWave < kStepPages * (kMaxPrefixSteps + 4) && tid < 4 * kStepPages) sh.page[kStepPages * kMaxPrefixSteps + tid] = -1;
             const unsigned long long bad_lanes = __builtin_amdgcn_ballot_w64(bad);
             if (bad_lanes != 0 && kvh == 0 && row_block == 0 && lane == 0 && p.errors != nullptr)
                 atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad_lanes));
         }
         __syncthreads();
 
-        // Wavefront w brings in page w of a step.
+        // Wavefront w brings in page w of a step (of eight: half of page w / 2).
+        static_assert(N % kPerPage == 0, "whole pieces");
+        constexpr int PN = N / kPerPage;
+        const int my_page = wave / kPerPage, j0 = wave % kPerPage * PN;
         const char *khead = static_cast<const char *>(p.k_cache) + (size_t)kvh * kPageBytes;
         const char *vhead = static_cast<const char *>(p.v_cache) + (size_t)kvh * kPageBytes;
         const uint32_t page_stride = (uint32_t)p.Hkv * kPageBytes;
         struct {
-            u32x4 k[N], v[N];
+            u32x4 k[PN], v[PN];
             float scale;   // 8-bit: the page's record, an entry per lane
         } in;
         auto load = [&](int page_entry) {
@@ -1056,10 +1061,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             const __amdgpu_buffer_rsrc_t kd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(khead + at), 0, bytes, kBufferFlags);
             const __amdgpu_buffer_rsrc_t vd = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(vhead + at), 0, bytes, kBufferFlags);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                in.k[j] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, j * 64, 0)
-                             : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, j * 1024, 0);
-                in.v[j] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, j * 1024, 0);
+            for (int i = 0; i < PN; ++i) {
+                in.k[i] = TM ? __builtin_amdgcn_raw_buffer_load_b128(kd, n16 * (D * 2) + g * 16, (j0 + i) * 64, 0)
+                             : __builtin_amdgcn_raw_buffer_load_b128(kd, lane * 16, (j0 + i) * 1024, 0);
+                in.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vd, lane * 16, (j0 + i) * 1024, 0);
             }
             if constexpr (B8) {
                 const __amdgpu_buffer_rsrc_t sd = __builtin_amdgcn_make_buffer_rsrc(
@@ -1068,36 +1073,37 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             }
         };
         auto store = [&](int buf) {
-            unsigned char *ks = sh.k[buf] + (wave >> 1) * (KS * 1024) + (wave & 1) * 256, *vs = sh.v[buf];
+            unsigned char *ks = sh.k[buf] + (my_page >> 1) * (KS * 1024) + (my_page & 1) * 256, *vs = sh.v[buf];
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
+            for (int i = 0; i < PN; ++i) {
+                const int j = j0 + i;
                 if constexpr (B8) {   // token n16, dims 64 j + 16 g .. + 15; tokens 4 g .. + 3, dims 64 j + 16 e + n16
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const u32x2 a = codes_to_bf16<INT8>(in.k[j][2 * e]), b = codes_to_bf16<INT8>(in.k[j][2 * e + 1]);
+                        const u32x2 a = codes_to_bf16<INT8>(in.k[i][2 * e]), b = codes_to_bf16<INT8>(in.k[i][2 * e + 1]);
                         *reinterpret_cast<u32x4 *>(ks + (4 * j + g) * 1024 + (e * 32 + n16) * 16) = (u32x4){a.x, a.y, b.x, b.y};
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<u32x2 *>(vs + (wave * SL + 2 * j + e / 2) * 1024 + ((g & 1) * 32 + (e % 2) * 16 + n16) * 16 + (g >> 1) * 8) =
-                            codes_to_f16<INT8>(in.v[j][e]);
+                        *reinterpret_cast<u32x2 *>(vs + (my_page * SL + 2 * j + e / 2) * 1024 + ((g & 1) * 32 + (e % 2) * 16 + n16) * 16 + (g >> 1) * 8) =
+                            codes_to_f16<INT8>(in.v[i][e]);
                 } else {              // token n16, dims 32 j + 8 g .. + 7
-                    *reinterpret_cast<u32x4 *>(ks + (2 * j + (g >> 1)) * 1024 + ((g & 1) * 32 + n16) * 16) = in.k[j];
+                    *reinterpret_cast<u32x4 *>(ks + (2 * j + (g >> 1)) * 1024 + ((g & 1) * 32 + n16) * 16) = in.k[i];
                     if constexpr (TM) {
                         constexpr int LR = D / 8;   // lanes per token row of a 1 KB load
-                        *reinterpret_cast<u32x4 *>(vs + (wave * SPEC_BLOCK_SIZE + (kWave / LR) * j + lane / LR) * v_row_bytes(D) + (lane % LR) * 16) = in.v[j];
+                        *reinterpret_cast<u32x4 *>(vs + (my_page * SPEC_BLOCK_SIZE + (kWave / LR) * j + lane / LR) * v_row_bytes(D) + (lane % LR) * 16) = in.v[i];
                     } else {          // tokens 4 g .. + 3, dims 32 j + 16 e + n16
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
-                            *reinterpret_cast<u32x2 *>(vs + (wave * SL + j) * 1024 + ((g & 1) * 32 + e * 16 + n16) * 16 + (g >> 1) * 8) =
-                                (u32x2){in.v[j][2 * e], in.v[j][2 * e + 1]};
+                            *reinterpret_cast<u32x2 *>(vs + (my_page * SL + j) * 1024 + ((g & 1) * 32 + e * 16 + n16) * 16 + (g >> 1) * 8) =
+                                (u32x2){in.v[i][2 * e], in.v[i][2 * e + 1]};
                     }
                 }
             }
             if constexpr (B8) {
-                if (lane < 32) {   // 16 scales of K, 16 of V (a page that reads as zeros: the smallest one)
+                if (lane < 32 && wave % kPerPage == 0) {   // 16 scales of K, 16 of V (a page that reads as zeros: the smallest one)
                     const float x = __builtin_elementwise_maximum(in.scale, kSmallestScale);
-                    float *to = &sh.scale[buf][0][wave * 16 + n16];
+                    float *to = &sh.scale[buf][0][my_page * 16 + n16];
                     constexpr int kRow = kStepPages * SPEC_BLOCK_SIZE;
                     if (lane < 16) to[0] = in.scale * p.scale_log2;
                     else {
@@ -1225,10 +1231,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             }
         };
 
-        load(sh.page[wave]);
+        load(sh.page[my_page]);
         store(0);
-        load(sh.page[kStepPages + wave]);
-        int entry_ahead = sh.page[2 * kStepPages + wave];
+        load(sh.page[kStepPages + my_page]);
+        int entry_ahead = sh.page[2 * kStepPages + my_page];
         for (int u = 0; u < steps; ++u) {
             const int buf = u & 1;
             __syncthreads();        // step u is in LDS, and no wavefront reads step u - 1 any more
@@ -1236,7 +1242,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_rows_kernel(CacheAttnParam
             for (int i = 0; i < kAhead; ++i) operand[i] = read_k(buf, i);
             store(buf ^ 1);
             load(entry_ahead);
-            entry_ahead = sh.page[kStepPages * (u + 3) + wave];
+            entry_ahead = sh.page[kStepPages * (u + 3) + my_page];
             scores(buf);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) operand[i] = read_v(buf, i);
@@ -1310,7 +1316,7 @@ template <int KIND, int NT, int D, bool FULL>
 void go(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
 {
     if (at.many_rows) {
-        if constexpr (NT == 1) hipLaunchKernelGGL((prefix_rows_kernel<KIND, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p);
+        if constexpr (NT == 1 || (NT == 2 && D == 128)) hipLaunchKernelGGL((prefix_rows_kernel<KIND, D, FULL, 4 * NT>), at.blocks, dim3(4 * NT * kWave), 0, stream, p);
         return;
     }
     hipLaunchKernelGGL((cache_attn_kernel<KIND, NT, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p, at.prefix);
@@ -1356,7 +1362,7 @@ hipError_t launch_cache_attn(const CacheAttnParams &p, hipStream_t stream)
 {
     if (p.max_prefix_chunks > 0) {
         const dim3 blocks = p.prefix_many_rows ? dim3(p.prefix_row_blocks) : dim3(p.Hkv, p.prefix_row_blocks, p.max_prefix_chunks);
-        const hipError_t err = launch_kind(p, p.prefix_many_rows ? 1 : p.prefix_tiles, CacheLaunch{blocks, 1, p.prefix_many_rows}, stream);
+        const hipError_t err = launch_kind(p, p.prefix_many_rows ? p.prefix_rows_log2 - 6 : p.prefix_tiles, CacheLaunch{blocks, 1, p.prefix_many_rows}, stream);
         if (err != hipSuccess) return err;
     }
     return launch_kind(p, p.row_tiles, CacheLaunch{dim3(p.Hkv, p.B, p.row_blocks * p.max_chunks), 0, 0}, stream);

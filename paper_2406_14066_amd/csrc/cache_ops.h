@@ -50,7 +50,7 @@ hipError_t launch_kv8_read(const Kv8ReadParams &p, hipStream_t stream);
 // in fp32 (prefixes with many rows and a bf16 output: acc in fp16).
 constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's four wavefronts: 64 pages each
 
-constexpr int kPrefixRows = 128;        // many rows: rows of a row block
+constexpr int kPrefixRows = 32;         // many rows: rows of a wavefront; a block has 4 of them, or 8
 constexpr int kStepPages = 4;           // ... pages of a step
 constexpr int kMaxPrefixSteps = 64;     // ... most steps of a block
 
@@ -64,6 +64,7 @@ struct CacheAttnParams {
     int32_t prefix_tiles, prefix_row_blocks;    // prefix: 16-row tiles of a block, blocks over all groups
     int32_t prefix_chunk_tokens, max_prefix_chunks;   // 0: no group has a prefix
     int32_t prefix_many_rows, prefix_piece_steps;   // the launch for many rows: steps of a block, prefix_row_blocks blocks
+    int32_t prefix_rows_log2;                   // ... log2 of a block's rows
     int32_t prefix_capacity;                    // longest prefix planned for
     int32_t max_q_rows;                         // rows of the largest request
     uint32_t generation;

@@ -39,7 +39,7 @@ def test_cache_kernels_use_no_private_memory_and_two_wavefronts_fit_a_simd(tmp_p
         if m and name is not None:
             kernels[name][m.group(1).split(" ")[0]] = int(m.group(2))
     count = lambda part: sum(part in k for k in kernels)
-    assert (count("cache_attn_kernel"), count("prefix_rows_kernel"), count("kv8_append_kernel"), count("kv8_read_kernel")) == (48, 16, 8, 8)
+    assert (count("cache_attn_kernel"), count("prefix_rows_kernel"), count("kv8_append_kernel"), count("kv8_read_kernel")) == (48, 24, 8, 8)
     for name, r in kernels.items():
         assert r["ScratchSize"] == 0, name
         assert r["Occupancy"] >= 2, (name, r)
