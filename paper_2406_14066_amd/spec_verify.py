@@ -400,7 +400,12 @@ def _check_tokens(t, like=None):
         raise ValueError("rows must be [T, heads, d] with contiguous heads")
     if like is not None and (t.shape != like.shape or t.dtype != like.dtype or (t.shape[0] > 1 and t.stride(0) != like.stride(0))):
         raise ValueError("rows must agree in shape, dtype and token stride")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    row = t.shape[1] * t.shape[2]
+    if t.shape[0] <= 1:
+        return row
+    if t.stride(0) < row:   # (0, of an expanded tensor, means packed rows in the argument structs)
+        raise ValueError("tokens must not lie on each other")
+    return t.stride(0)
 
 
 def _check_pools(k_cache, v_cache, kv_scale):
