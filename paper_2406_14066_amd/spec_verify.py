@@ -420,6 +420,24 @@ def _check_pools(k_cache, v_cache, kv_scale):
     return nb, Hkv, d
 
 
+def _check_arrays(like, block_table, hc, hk, error_count, tensors, arrays):
+    """What the kernels index by request or group: [B, n] block table and `arrays` of (tensor, least entries), packed int32 on the pools'
+    device, where `tensors` are too."""
+    import torch
+    B = hc.shape[0] - 1
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_blocks_per_req]")
+    if hk is not None and hk.shape[0] < B:
+        raise ValueError("host_kv_len must have an entry per request")
+    for t, n in ((block_table, B * block_table.shape[1]),) + tuple(arrays):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n or t.device != like.device):
+            raise ValueError("index arrays must be contiguous int32 on the pools' device, an entry per request or group")
+    if error_count is not None and (error_count.dtype != torch.int64 or error_count.numel() < 1 or error_count.device != like.device):
+        raise ValueError("error_count must be int64 on the pools' device")
+    if any(t is not None and t.device != like.device for t in tensors):
+        raise ValueError("all tensors must be on the pools' device")
+
+
 def alloc_kv8_pools(num_blocks: int, Hkv: int, d: int, kv_dtype, device="cuda"):
     """(k_cache, v_cache, kv_scale) of an 8-bit cache; kv_dtype is torch.float8_e4m3fn or torch.int8."""
     import torch
@@ -439,7 +457,9 @@ def make_kv8_append_args(new_k, new_v, k_cache, v_cache, kv_scale, block_table, 
         raise ValueError("rows must be [T, %d, %d]" % (a.Hkv, a.d))
     _check_tokens(new_v)
     a.token_stride = _check_tokens(new_k, new_v)
-    a.T, a.B = new_k.shape[0], hc.shape[0] - 1
+    B = hc.shape[0] - 1
+    _check_arrays(k_cache, block_table, hc, hk, error_count, (new_k, new_v, v_cache, kv_scale), ((kv_len, B), (cu_q_len, B + 1)))
+    a.T, a.B = new_k.shape[0], B
     a.max_blocks_per_req = block_table.shape[1]
     a.src_dtype = _type_of(new_k, SPEC_F32, SPEC_BF16)
     a.kv_dtype = _type_of(k_cache, SPEC_E4M3, SPEC_INT8)
@@ -465,7 +485,9 @@ def make_kv8_read_args(out_k, out_v, k_cache, v_cache, kv_scale, block_table, st
     for out in (out_k, out_v):
         if tuple(out.shape[1:]) != (a.Hkv, a.d) or not out.is_contiguous() or out.shape != out_k.shape or out.dtype != out_k.dtype:
             raise ValueError("out_k and out_v must be contiguous [T, %d, %d]" % (a.Hkv, a.d))
-    a.T, a.B = out_k.shape[0], hc.shape[0] - 1
+    B = hc.shape[0] - 1
+    _check_arrays(k_cache, block_table, hc, None, error_count, (out_k, out_v, v_cache, kv_scale), ((start, B), (cu_len, B + 1)))
+    a.T, a.B = out_k.shape[0], B
     a.max_blocks_per_req = block_table.shape[1]
     a.kv_dtype = _type_of(k_cache, SPEC_E4M3, SPEC_INT8)
     a.out_dtype = _type_of(out_k, SPEC_F32, SPEC_BF16)
@@ -481,7 +503,8 @@ def spec_kv8_read(args: Kv8ReadArgs, stream=None) -> None:
     _check(lib().spec_kv8_read(C.byref(args), _stream_handle(stream)), "spec_kv8_read")
 
 
-def _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count):
+def _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count,
+               groups=()):
     a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, v_cache, kv_scale)
     _type_of(q, SPEC_BF16)
     a.q_token_stride = _check_tokens(q)
@@ -489,6 +512,7 @@ def _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, 
     if q.shape[2] != a.d or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("q and out must be [T, Hq, %d], out contiguous" % a.d)
     a.B = hc.shape[0] - 1
+    _check_arrays(k_cache, block_table, hc, hk, error_count, (q, v_cache, kv_scale, out), ((kv_len, a.B), (cu_q_len, a.B + 1)) + groups)
     a.max_blocks_per_req = block_table.shape[1]
     a.out_dtype = _type_of(out, SPEC_F32, SPEC_BF16)
     a.max_kv_len = max_kv_len
@@ -538,7 +562,8 @@ def make_prefix_attn_args(q, k_cache, v_cache, block_table, kv_len, cu_q_len, cu
     if hg.shape[0] != hp.shape[0] + 1:
         raise ValueError("cu_group must have one entry more than prefix_len")
     a = PrefixAttnArgs()
-    _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count)
+    _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count,
+               ((cu_group, hg.shape[0]), (prefix_len, hp.shape[0])))
     a.kv_dtype = _type_of(k_cache, SPEC_BF16, SPEC_E4M3, SPEC_INT8)
     a.kv_layout = kv_layout
     a.G = hp.shape[0]
