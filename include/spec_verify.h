@@ -328,7 +328,8 @@ spec_status spec_kv_repack_mfma(const void *src_k, const void *src_v, void *dst_
  *   code = round(x * (M / a)),  scale = a / M,  a = max(largest |x| of the row's d elements, 2^-60)
  *
  * with M = 448 for SPEC_E4M3 (8-bit floating point, 4 exponent and 3 mantissa bits, no infinities) and 127 for
- * SPEC_INT8, rounded to nearest, ties to even; the value of a code is code * scale.  The fp32 steps are M * (1 / a) and a * (1 / M).  A row that holds a NaN or an infinity
+ * SPEC_INT8, rounded to nearest, ties to even; the value of a code is code * scale.  The fp32 steps are M * (1 / a), 1 / a with all of fp32's significant bits
+ * whatever its size, and a * (1 / M).  A row that holds a NaN or an infinity
  * has no scale: its scale is NaN and its codes are 0, so it reads back as NaN and so does every attention row
  * that sees it (rows that do not see it are not touched).
  *

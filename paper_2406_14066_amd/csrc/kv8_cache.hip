@@ -95,9 +95,11 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
         }
         const bool finite = most < 0x7F800000u;
         const float a = fmaxf(__uint_as_float(most), kSmallestRow);
-        // (the two quotients as products with rounded reciprocals, as fp32 tensor arithmetic does them: codes at a tie agree with it)
+        // (the two quotients as products with rounded reciprocals, as fp32 tensor arithmetic does them: codes at a tie agree with it;
+        // 1 / a as 2^8 times itself, which has the same bits and is a normal number for every a: above 2^126 1 / a is not, and denormals
+        // are flushed)
         scale[kv] = finite ? a * (1.0f / kMost) : __uint_as_float(0x7FC00000u);
-        const float inv = kMost * (1.0f / a);
+        const float inv = kMost * 0x1p-8f * (1.0f / (a * 0x1p-8f));
         uint32_t code[N / 4];
 #pragma unroll
         for (int j = 0; j < N / 4; ++j) {
