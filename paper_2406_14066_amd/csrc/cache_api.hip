@@ -368,12 +368,16 @@ Plan make_plan(const spec_prefix_attn_args *a)
     return pl;
 }
 
+// Tag of a call's tickets (see ticket_arrive).  The workspace may hold what any other call left in it, partial results above all, so
+// the tags are bits that no fp32 result has: negative NaNs whose lower half is not zero (arithmetic makes 0x7FC00000, or hands on
+// the NaN of a bf16 input).  They recur after 8 million calls, which leaves nothing behind: the last block to arrive clears its ticket.
 uint32_t next_generation()
 {
-    static std::atomic<uint32_t> counter{0x40000000u};
-    uint32_t g = ++counter;
-    if (g == 0) g = ++counter;
-    return g;
+    static std::atomic<uint32_t> calls{0u};
+    for (;;) {
+        const uint32_t tag = 0xFF800000u | (calls++ & 0x007FFFFFu);
+        if ((tag & 0xFFFFu) != 0) return tag;
+    }
 }
 
 spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
