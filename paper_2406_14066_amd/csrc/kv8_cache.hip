@@ -182,6 +182,10 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_read_kernel(Kv8ReadPara
         k[i] = *reinterpret_cast<const u32x4 *>(kp + i * 1024 + lane * 16);   // token n16, dims 64 i + 16 g .. + 15
         v[i] = *reinterpret_cast<const u32x4 *>(vp + i * 1024 + lane * 16);   // tokens 4 g .. + 3, dims 64 i + 16 q + n16
     }
+    if (!there) {   // (not some other page times zero: that page may hold anything)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) k[i] = v[i] = (u32x4){0u, 0u, 0u, 0u};
+    }
     const float ks = there ? sc[n16] : 0.0f;
     const f32x4 vs = there ? *reinterpret_cast<const f32x4 *>(sc + 16 + 4 * g) : (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     unsigned char *st = stage[threadIdx.x / kWave];

@@ -56,3 +56,21 @@ def test_codes_do_not_depend_on_the_magnitude_of_the_row(kv, src):
         value = R.code_value(codes.view(np.uint8), kv) * got_scales.astype(np.float64)[..., None]
         np.testing.assert_array_equal(back, value.astype(np.float32))
         assert np.isfinite(back).all()
+
+
+@pytest.mark.parametrize("kv", KINDS)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_tokens_that_do_not_exist_read_as_zeros_whatever_the_pool_holds(kv, out):
+    """Every byte of the pool is a code, NaN's among them: a page outside the pool is not some other page times zero."""
+    Hkv, d, n = 3, 128, 40
+    pools = [torch.full((4, Hkv, 16, d), 0x7F, dtype=torch.int8, device="cuda").view(_type(kv)) for _ in range(2)]
+    scale = torch.full((4, Hkv, 2, 16), float("inf"), device="cuda")
+    table = torch.tensor([[9, -1, 4]], dtype=torch.int32, device="cuda")
+    cu = np.array([0, n], dtype=np.int32)
+    outs = [torch.full((n, Hkv, d), 7.0, dtype=torch.float32 if out == "f32" else torch.bfloat16, device="cuda") for _ in range(2)]
+    errors = torch.zeros(1, dtype=torch.int64, device="cuda")
+    args, keep = sv.make_kv8_read_args(*outs, *pools, scale, table, None, torch.from_numpy(cu).cuda(), cu, error_count=errors)
+    sv.spec_kv8_read(args)
+    torch.cuda.synchronize()
+    assert int(errors.item()) == n
+    assert bool((outs[0] == 0).all()) and bool((outs[1] == 0).all())
