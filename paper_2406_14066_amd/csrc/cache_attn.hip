@@ -854,45 +854,23 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
         auto add_pieces = [&](auto count, int c0) {
             constexpr int U = decltype(count)::value;
             f32x2 ml[NT][U];
-            u32x4 o[NT][U][SN];   // as they were stored
-            constexpr int kHalves = SN == 2 ? 1 : 0;   // (fp16: a lane's two slices are 16 bytes)
-            const bool halves = !FULL && many;
+            f32x4 o[NT][U][SN];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const size_t slot = rh[nt] * p.max_prefix_chunks + min(c0 + u, w.prefix_chunks - 1);
+                    const float *from = p.prefix_acc + slot * D;
                     ml[nt][u] = *reinterpret_cast<const f32x2 *>(p.prefix_ml + slot * 2);
-                    if (halves) {
-                        const _Float16 *from = reinterpret_cast<const _Float16 *>(p.prefix_acc) + slot * D + partial_place<D>(dim0);
-                        if constexpr (kHalves) {
-                            o[nt][u][0] = *reinterpret_cast<const u32x4 *>(from);
-                        } else {
-                            const u32x2 x = *reinterpret_cast<const u32x2 *>(from);
-                            o[nt][u][0] = (u32x4){x.x, x.y, 0u, 0u};
-                        }
-                    } else {
-                        const float *from = p.prefix_acc + slot * D;
 #pragma unroll
-                        for (int i = 0; i < SN; ++i)
-                            o[nt][u][i] = *reinterpret_cast<const u32x4 *>(from + (many ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
-                    }
+                    for (int i = 0; i < SN; ++i)
+                        o[nt][u][i] = *reinterpret_cast<const f32x4 *>(from + (many ? partial_place<D>(dim0) + 4 * i : dim0 + i * 16));
                 }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    f32x4 x[SN];
-                    if (halves) {
-#pragma unroll
-                        for (int i = 0; i < SN; ++i)
-                            x[i] = __builtin_convertvector(__builtin_bit_cast(f16x4, (u32x2){o[nt][u][0][2 * i], o[nt][u][0][2 * i + 1]}), f32x4);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < SN; ++i) x[i] = __builtin_bit_cast(f32x4, o[nt][u][i]);
-                    }
-                    if (c0 + u < w.prefix_chunks) sum[nt].add(ml[nt][u].x, ml[nt][u].y, x);
-                }
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u < w.prefix_chunks) sum[nt].add(ml[nt][u].x, ml[nt][u].y, o[nt][u]);
         };
         for (int c0 = 0; c0 < w.prefix_chunks;) {
             if (w.prefix_chunks - c0 > kFew) {
@@ -1255,33 +1233,11 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
 
         // The rows' partial results, half of the dims at a time through LDS so that they go out in long pieces.
         l_run += __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false)[half ^ 1]);
-        if constexpr (!FULL) {
-            // As fp16, whose rounding (2^-12 of a value, or of 2^-14 of the row's largest) is small beside that of the bf16
-            // output: half the bytes to write here and to read back.  The row's reference takes the power of two that
-            // brings its largest finite value to at most one.
-            float most = 0.0f;
-#pragma unroll
-            for (int sl = 0; sl < SL; ++sl)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float x = __builtin_fabsf(acc[sl][e]);
-                    most = x < INFINITY && x > most ? x : most;
-                }
-            most = max_across_xor32(most);
-            const int up = __builtin_amdgcn_frexp_expf(most);
-            m_run += (float)up;
-            l_run = __builtin_amdgcn_ldexpf(l_run, -up);
-#pragma unroll
-            for (int sl = 0; sl < SL; ++sl)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[sl][e] = __builtin_amdgcn_ldexpf(acc[sl][e], -up);
-        }
         if (half == 0 && c32 < rows)
             *reinterpret_cast<f32x2 *>(p.prefix_ml + (out_index(c32) * p.max_prefix_chunks + slot) * 2) = (f32x2){m_run, l_run};
         __syncthreads();
         unsigned char *o = sh.o[wave];
-        constexpr int kPartial = FULL ? 4 : 2;        // bytes of a value
-        constexpr int OP = D / 2 * kPartial / 16;     // 16-byte pieces of half a row
+        constexpr int OP = D / 2 * 4 / 16;            // 16-byte pieces of half a row
 #pragma unroll
         for (int d2 = 0; d2 < 2; ++d2) {   // (a region for each wavefront, and LDS executes a wavefront's accesses in order)
 #pragma unroll
@@ -1290,9 +1246,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
                 for (int i = 0; i < 4; ++i) {
                     const f32x16 &x = acc[d2 * (SL / 2) + sl];
                     const f32x4 four = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                    unsigned char *at4 = o + c32 * Sh::kOutRow + partial_place<D>(32 * sl + 8 * i + 4 * half) * kPartial;
-                    if constexpr (FULL) *reinterpret_cast<f32x4 *>(at4) = four;
-                    else *reinterpret_cast<f16x4 *>(at4) = __builtin_convertvector(four, f16x4);
+                    *reinterpret_cast<f32x4 *>(o + c32 * Sh::kOutRow + partial_place<D>(32 * sl + 8 * i + 4 * half) * 4) = four;
                 }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -1301,8 +1255,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
             for (int piece = lane; piece < 32 * OP; piece += kWave) {
                 const int r = piece / OP, c = piece % OP;
                 if (r < rows)
-                    *reinterpret_cast<u32x4 *>(reinterpret_cast<unsigned char *>(p.prefix_acc) +
-                                               ((out_index(r) * p.max_prefix_chunks + slot) * D + d2 * (D / 2)) * kPartial + c * 16) =
+                    *reinterpret_cast<u32x4 *>(p.prefix_acc + (out_index(r) * p.max_prefix_chunks + slot) * D + d2 * (D / 2) + c * 4) =
                         *reinterpret_cast<const u32x4 *>(o + r * Sh::kOutRow + c * 16);
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

@@ -47,7 +47,7 @@ hipError_t launch_kv8_read(const Kv8ReadParams &p, hipStream_t stream);
 //            writes the output; otherwise the last of its blocks to finish joins its partials first (tickets).
 // Partial results of query row r (token row * Hq + head), chunk (or piece) c:
 //   acc [r][max chunks][d]  sum_t 2^(x_t - m) V_t, un-normalised    ml [r][max chunks][2]  m and sum_t 2^(x_t - m)
-// in fp32 (prefixes with many rows and a bf16 output: acc in fp16).
+// in fp32.
 constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's four wavefronts: 64 pages each
 
 constexpr int kPrefixRows = 32;         // many rows: rows of a wavefront; a block has 4 of them, or 8
