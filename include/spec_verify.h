@@ -433,8 +433,7 @@ typedef struct {
     int32_t G;                    /* groups, G >= 1 */
     int32_t kv_dtype;             /* SPEC_BF16, SPEC_E4M3 or SPEC_INT8 */
     int32_t kv_layout;            /* SPEC_BF16: spec_kv_layout; 8-bit pools: SPEC_KV_MFMA */
-    int32_t out_dtype;            /* SPEC_F32: softmax weights as two (bf16 pools: three) 16-bit terms; SPEC_BF16: as one (bf16 pools: two,
-                                     but one in the launch for prefixes with more than 48 query rows) */
+    int32_t out_dtype;            /* SPEC_F32: softmax weights as two (bf16 pools: three) 16-bit terms; SPEC_BF16: as one (bf16 pools: two) */
     int32_t max_kv_len;           /* length bucket, as in spec_attn_args: the lengths in kv_len may change under a captured
                                      launch; the groups and their prefixes are part of the plan */
     int64_t q_token_stride;       /* as in spec_kv8_attn_args */

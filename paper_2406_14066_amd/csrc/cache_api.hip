@@ -221,7 +221,7 @@ constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kWideStep
 template <typename F>
 int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, bool wide, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
 {
-    const double units = compute_units(), slots = wide ? units : 2 * units, busy_us = wide ? kWideStepUs : kSharedStepUs, factor = d / 128.0 * (full ? (codes ? 1.5 : 2.0) : 1.0);   // (more terms: more products with V)
+    const double units = compute_units(), slots = wide ? units : 2 * units, busy_us = wide ? kWideStepUs : kSharedStepUs, factor = d / 128.0 * (codes ? (full ? 1.5 : 1.0) : (full ? 2.0 : 1.45));   // (more terms: more products with V)
     int best = std::min(most_steps, kMaxPrefixSteps);
     best_us = 1e30;
     for (int len = best; len >= 1; len = std::min(len - 1, len * 7 / 8)) {

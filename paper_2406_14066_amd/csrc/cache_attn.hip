@@ -951,7 +951,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
     constexpr int KS = D / 16, SL = D / 32;
     constexpr int kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);
     constexpr int N = B8 ? D / 64 : D / 32;              // 1 KB pieces of a page's K, of its V
-    constexpr int TERMS = FULL ? (B8 ? 2 : 3) : 1;
+    constexpr int TERMS = FULL ? (B8 ? 2 : 3) : (B8 ? 1 : 2);   // as in cache_attn_kernel: a row's error does not depend on the kernel that takes it
     constexpr float kTop = B8 ? 7.0f : 0.0f;
     typedef std::conditional_t<B8, f16x8, bf16x8> Weights;
     typedef RowsShared<KIND, D, W> Sh;
@@ -1176,7 +1176,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
                     const float x = s[h][4 * i + r];
                     const float e = fast_exp2(B8 ? x - m_run : fmaf(x, p.scale_log2, -m_run));
                     if constexpr (B8) l_run = fmaf(e, rv[r], l_run);
-                    else if constexpr (FULL) l_run += e;
+                    else l_run += e;
                     float rest = e;
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t) {
@@ -1184,13 +1184,6 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
                         rest -= (float)pw[h][i / 2][t][4 * (i % 2) + r];
                     }
                 }
-            }
-            if constexpr (!B8 && !FULL) {   // the sum of the weights as they are multiplied, two at a time
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2)
-                        l_run = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){pw[h][i][0][e], pw[h][i][0][e + 1]}, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, l_run, false);
             }
         };
         // product of pair h's weights with its V in buffer `buf`
