@@ -10,7 +10,9 @@
 //   x_t = (q . K_t) k_t softmax_scale log2 e,   y_t = x_t + log2 v_t,   w_t = 2^(y_t - m),  m: running maximum of y
 //   O = sum w_t V_t,   l = sum w_t / v_t
 // so that the weights of the product are at most one whatever the scales are, and V's scale costs an addition in
-// the exponent; they fit fp16, whose 11 bits keep their rounding (2^-12) below that of a bf16 output.
+// the exponent; they fit fp16, whose 11 bits keep their rounding (2^-12) below that of a bf16 output.  l is kept times 2^22: 2^22 / v_t is
+// between 2^-99 and 2^91, so that weights from 2^-34 of the largest on up to those of a million tokens stay normal numbers in it
+// whatever the scales are (denormals are flushed).
 #include "code8.h"
 
 #include <math.h>
@@ -40,6 +42,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kDeviceScope = 16;        // "sc1" bit of a raw buffer access: coherent over the device's caches
 constexpr float kRescaleSlack = 8.0f;   // the running reference follows the maximum when it is this much behind
+constexpr float kLift = 0x1p22f, kLower = 0x1p-22f;   // 8-bit pages: of the sums of weights (see above)
 
 // Partial results of the launch for many rows keep a row's dims in the order in which the wavefronts that merge them hold
 // them: four groups of 4 from each 16-dim slice of a wavefront (D = 128: two slices), a lane's dims side by side.
@@ -532,7 +535,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
             }
         }
         load_k(i + 1);
-        // to base-2 exponents; per token: k = scale of x, lv = log2 of V's scale, rv = its reciprocal (each made by one lane of
+        // to base-2 exponents; per token: k = scale of x, lv = log2 of V's scale, rv = its lifted reciprocal (each made by one lane of
         // the row and handed to the others)
         f32x4 ks[2], lv[2], rv[2];
         if constexpr (B8) {
@@ -542,7 +545,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
                 k1 = on ? k1 : 0.0f;
                 v1 = on ? v1 : kSmallestScale;
             }
-            const float l1 = __builtin_amdgcn_logf(v1), r1 = __builtin_amdgcn_rcpf(v1);
+            const float l1 = __builtin_amdgcn_logf(v1), r1 = __builtin_amdgcn_rcpf(v1 * kLower);
             auto hand_out = [&](float x, f32x4(&to)[2]) {
                 to[0] = (f32x4){row_broadcast<0>(x), row_broadcast<1>(x), row_broadcast<2>(x), row_broadcast<3>(x)};
                 to[1] = (f32x4){row_broadcast<4>(x), row_broadcast<5>(x), row_broadcast<6>(x), row_broadcast<7>(x)};
@@ -885,7 +888,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         if (!on[nt]) continue;
-        const float inv = sum[nt].l == 0.0f ? 0.0f : 1.0f / sum[nt].l;   // (a row that has seen no key is zero)
+        const float inv = sum[nt].l == 0.0f ? 0.0f : (B8 ? kLift : 1.0f) / sum[nt].l;   // (a row that has seen no key is zero)
 #pragma unroll
         for (int i = 0; i < SN; ++i) {
             const f32x4 o = sum[nt].o[i] * inv;
@@ -937,7 +940,7 @@ struct RowsShared {
         };
         alignas(16) unsigned char o[W][kPrefixRows * kOutRow];   // results on their way out, by half rows
     };
-    // 8-bit pages, per token: K's scale with the softmax scale, log2 of V's, its reciprocal
+    // 8-bit pages, per token: K's scale with the softmax scale, log2 of V's, its lifted reciprocal
     float scale[is_8bit(KIND) ? 2 : 1][3][is_8bit(KIND) ? kStepPages * SPEC_BLOCK_SIZE : 1];
     int page[kStepPages * (kMaxPrefixSteps + 4)];   // the steps' block-table entries, and four more steps'; -1: outside the pool, or past the end
     static_assert(kStepPages * kMaxPrefixSteps <= W * kWave, "a thread per page");
@@ -1086,7 +1089,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
                     if (lane < 16) to[0] = in.scale * p.scale_log2;
                     else {
                         to[kRow] = __builtin_amdgcn_logf(x);
-                        to[2 * kRow] = __builtin_amdgcn_rcpf(x);
+                        to[2 * kRow] = __builtin_amdgcn_rcpf(x * kLower);
                     }
                 }
             }

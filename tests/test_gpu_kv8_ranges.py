@@ -1,4 +1,4 @@
-"""The 8-bit cache at the ends of the number range."""
+"""The 8-bit cache at the ends of the number range: rows of any finite magnitude, V scales of any size, pools that hold anything."""
 import numpy as np
 import pytest
 import torch
@@ -74,3 +74,56 @@ def test_tokens_that_do_not_exist_read_as_zeros_whatever_the_pool_holds(kv, out)
     torch.cuda.synchronize()
     assert int(errors.item()) == n
     assert bool((outs[0] == 0).all()) and bool((outs[1] == 0).all())
+
+
+@pytest.mark.parametrize("shared", [None, 1, 0], ids=["kv8", "shared", "whole"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("kv", KINDS)
+@pytest.mark.parametrize("power", [-60, 0, 60, 119])
+@pytest.mark.parametrize("rows", [30, 60], ids=["few", "many"])
+def test_small_weights_count_whatever_the_scale_of_v(rows, kv, out, power, shared, tuning):
+    """Every wavefront's pages hold a token with 2^16 times the weight of each of the others, whose sum is a thousandth of the whole."""
+    if shared is not None:
+        tuning("SPEC_VERIFY_PREFIX_SHARED", shared)
+    Hq = Hkv = 2
+    d, n, B = 64, 8192, rows
+    pages = n // 16
+    rng = np.random.default_rng(33)
+    code = rng.integers(1, 127, size=(2, pages, Hkv, 16 * d)).astype(np.uint8)
+    code[0] = 0
+    one = 1 if kv == "int8" else 0x38                    # the value 1
+    code[0][:, :, R.cell(np.arange(16), 0, 0)] = one     # K is 1 in the first dim, and its scale the score
+    scales = np.full((pages, Hkv, 2, 16), 2.0 ** power, dtype=np.float32)
+    scales[:, :, 0] = 0.0
+    high = np.arange(pages) % 32 < 8
+    scales[high, :, 0, 5] = 16 * np.log(2.0)
+    dev = [torch.from_numpy(c.view(np.int8).reshape(pages, Hkv, 16, d)).cuda().view(_type(kv)) for c in code]
+    cu = np.arange(B + 1, dtype=np.int32)
+    kv_len = np.full(B, n, dtype=np.int32)
+    q = torch.zeros((B, Hq, d), device="cuda")
+    q[:, :, 0] = 1.0
+    q = q.to(torch.bfloat16)
+    o = torch.zeros((B, Hq, d), dtype=torch.float32 if out == "f32" else torch.bfloat16, device="cuda")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(B, 1)
+    arrays = (table, torch.from_numpy(kv_len).cuda(), torch.from_numpy(cu).cuda())
+    if shared is None:
+        args, keep = sv.make_kv8_attn_args(q, *dev, torch.from_numpy(scales).cuda(), *arrays, o, kv_len, cu, softmax_scale=1.0)
+        ws = sv.alloc_workspace(sv.spec_kv8_attn_workspace_bytes(args))
+        sv.spec_kv8_attn(args, ws)
+    else:                                                # (the last page is not the prefix's, and the same for all)
+        group, prefix = np.array([0, B], dtype=np.int32), np.array([n - 16], dtype=np.int32)
+        args, keep = sv.make_prefix_attn_args(q, *dev, *arrays, torch.from_numpy(group).cuda(), torch.from_numpy(prefix).cuda(), o, kv_len, cu, group,
+                                              prefix, kv_scale=torch.from_numpy(scales).cuda(), softmax_scale=1.0)
+        ws = sv.alloc_workspace(sv.spec_prefix_attn_workspace_bytes(args))
+        sv.spec_prefix_attn(args, ws)
+    torch.cuda.synchronize()
+    cache = np.moveaxis(np.array([R.token(code[1], scales, 1, t // 16, t % 16, kv) for t in range(n)]), 0, 1)     # [Hkv, n, d]
+    weight = np.ones(n)
+    weight.reshape(pages, 16)[high, 5] = 2.0 ** 16
+    want = (weight[None, :, None] * cache).sum(1) / weight.sum()
+    got = o.double().cpu().numpy()
+    # fp32 output: sums of 8192 terms (2^-24 of the sum each, as a random walk 2^-17.5) and weights of 22 bits: 2^-16 of the largest |v|;
+    # bf16: its own rounding (2^-8 of the value) and that of the weights as one fp16 (2^-11)
+    most = np.abs(cache).max()
+    limit = 2.0 ** -16 * most if out == "f32" else 2.0 ** -8 * np.abs(want) + 2.0 ** -11 * most
+    assert (np.abs(got - want[None]) <= limit).all(), np.abs(got / want[None] - 1).max()
