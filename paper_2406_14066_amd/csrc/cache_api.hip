@@ -385,7 +385,7 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     const Plan pl = make_plan(a);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
     if (a->B > 65535 || (!pl.prefix_many_rows && pl.prefix_row_blocks > 65535) || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
-    if (pl.blocks > kMaxPacked || pl.prefix_blocks > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if (pl.blocks > kMaxPacked || pl.prefix_blocks > (pl.prefix_many_rows ? kMaxPrefixBlocks : kMaxPacked)) return SPEC_EUNSUPPORTED;
     char *ws = static_cast<char *>(workspace);
     CacheAttnParams p;
     memset(&p, 0, sizeof p);

@@ -157,12 +157,13 @@ struct GroupWork {
         request = b0;
         row0 = p.cu_q_len[b0];
         const int end = p.cu_q_len[b1];
+        if (row0 < 0 || end <= row0 || end > p.T) return;
         rows = (end - row0) * p.group;
-        if (row0 < 0 || end > p.T || rows <= 0) return;
         pages = P / SPEC_BLOCK_SIZE;
         const int steps = (pages + kStepPages - 1) / kStepPages;
         pieces = (steps + p.prefix_piece_steps - 1) / p.prefix_piece_steps;
-        blocks = ((rows + (1 << p.prefix_rows_log2) - 1) >> p.prefix_rows_log2) * pieces;
+        // (more than there can be, from rows that several groups claim, stays more: sums of 64 of them do not wrap)
+        blocks = (int)min((int64_t)((rows + (1 << p.prefix_rows_log2) - 1) >> p.prefix_rows_log2) * pieces, (int64_t)kMaxPrefixBlocks + 1);
     }
     __device__ __forceinline__ void look(const CacheAttnParams &p, int g)
     {
@@ -193,9 +194,17 @@ __device__ __forceinline__ int group_blocks(const CacheAttnParams &p)
         work.look(p, base + threadIdx.x % kWave);
         int all;
         (void)running_sum(work.blocks, all);
-        total += all;
+        total = min(total + all, kMaxPrefixBlocks + 1);
     }
     return total;
+}
+
+// Row blocks of requests b0 .. b1 - 1 in the prefix launch for few rows, of `size` rows each; 0: none, or not valid.
+__device__ __forceinline__ int few_rows_blocks(const CacheAttnParams &p, int b0, int b1, int size)
+{
+    if (b0 < 0 || b0 > b1 || b1 > p.B) return 0;
+    const int row0 = p.cu_q_len[b0], end = p.cu_q_len[b1];
+    return row0 < 0 || end <= row0 || end > p.T ? 0 : ((end - row0) * p.group + size - 1) / size;
 }
 
 // One block of the own launch: grid (KV heads, requests, row blocks x chunks).
@@ -305,27 +314,16 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, Work &w)
     const int lane = threadIdx.x % kWave;
     int before = 0, g = -1;
     for (int base = 0; base < p.G && g < 0; base += kWave) {
-        int n = 0;
-        if (base + lane < p.G) {
-            const int b0 = p.cu_group[base + lane], b1 = p.cu_group[base + lane + 1];
-            if (b0 >= 0 && b0 <= b1 && b1 <= p.B) {
-                const int rows = (p.cu_q_len[b1] - p.cu_q_len[b0]) * p.group;
-                n = rows > 0 ? (rows + ROWS - 1) / ROWS : 0;
-            }
-        }
-        int sum = n;   // inclusive prefix sum over the lanes
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const int up = __shfl_up(sum, off);
-            if (lane >= off) sum += up;
-        }
+        const int n = base + lane < p.G ? few_rows_blocks(p, p.cu_group[base + lane], p.cu_group[base + lane + 1], ROWS) : 0;
+        int all;
+        const int sum = running_sum(n, all);
         const unsigned long long holds = __builtin_amdgcn_ballot_w64(before + sum > block);
         if (holds != 0) {
             const int at = __builtin_ctzll(holds);
             g = base + at;
             w.row_block = block - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(n, at));
         } else {
-            before += __builtin_amdgcn_readlane(sum, kWave - 1);
+            before += all;
         }
     }
     if (g < 0) return false;
@@ -336,7 +334,7 @@ __device__ __forceinline__ bool place_prefix(const CacheAttnParams &p, Work &w)
     w.b = b0;
     w.row0 = uniform_load(p.cu_q_len, b0);
     const int tokens = uniform_load(p.cu_q_len, b1) - w.row0;
-    if (!prefix_ok(p, P) || P == 0 || w.row0 < 0 || tokens < 0 || w.row0 + tokens > p.T) return false;   // (counted by the own launch)
+    if (!prefix_ok(p, P) || P == 0) return false;   // (counted by the own launch)
     w.rows = tokens * p.group;
     w.row_lo = w.row_block * ROWS;
     if (w.row_lo >= w.rows) return false;

@@ -53,6 +53,7 @@ constexpr int kMaxChunkTokens = 4096;   // the block-table entries of a block's 
 constexpr int kPrefixRows = 32;         // many rows: rows of a wavefront; a block has 4 of them, or 8
 constexpr int kStepPages = 4;           // ... pages of a step
 constexpr int kMaxPrefixSteps = 64;     // ... most steps of a block
+constexpr int kMaxPrefixBlocks = 1 << 24;   // ... most blocks of a launch
 
 struct CacheAttnParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, G;

@@ -56,8 +56,8 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_append_kernel(Kv8Append
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
     w.b = request_of_item(p.cu_q_len, p.B, item, items);
-    const int row0 = p.cu_q_len[w.b], n = p.cu_q_len[w.b + 1] - row0;
-    if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
+    const int row0 = p.cu_q_len[w.b], end = p.cu_q_len[w.b + 1], n = end - row0;
+    if (row0 < 0 || end <= row0 || end > p.T) return;
     const int pos0 = p.kv_len[w.b] - n;
     if (!place_page(w, pos0, n, row0, item - page_item(row0, w.b), p.block_table, p.max_blocks_per_req, p.num_blocks)) return;
 
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(kPageWaves *kWave) void kv8_read_kernel(Kv8ReadPara
     PageWork w;
     w.kvh = __builtin_amdgcn_readfirstlane(unit - item * p.Hkv);
     w.b = request_of_item(p.cu_len, p.B, item, items);
-    const int row0 = p.cu_len[w.b], n = p.cu_len[w.b + 1] - row0;
-    if (n <= 0 || row0 < 0 || row0 + n > p.T) return;
+    const int row0 = p.cu_len[w.b], end = p.cu_len[w.b + 1], n = end - row0;
+    if (row0 < 0 || end <= row0 || end > p.T) return;
     const int pos0 = p.start != nullptr ? p.start[w.b] : 0;
     if (!place_page(w, pos0, n, row0, item - page_item(row0, w.b), p.block_table, p.max_blocks_per_req, p.num_blocks)) return;
     if (w.page < 0 && w.kvh == 0 && lane == 0 && p.errors != nullptr) atomicAdd(p.errors, (unsigned long long)(w.s1 - w.s0));
