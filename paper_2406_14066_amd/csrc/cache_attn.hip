@@ -275,7 +275,19 @@ __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w
 {
     w.prefix_chunks = 0;
     if (w.prefix == 0) return true;
+    const bool first = w.chunk == 0 && w.kvh == 0 && w.row_block == 0;
     if (!p.prefix_many_rows) {
+        // (scalar loads, which do not wait for the pages)
+        const int b1 = uniform_load(p.cu_group, w.group_index + 1);
+        bool there = b1 > w.b && b1 <= p.B;
+        if (there) {
+            const int row0 = uniform_load(p.cu_q_len, w.head), end = uniform_load(p.cu_q_len, b1);
+            there = row0 >= 0 && row0 <= w.row0 && w.row0 + by_group(p, w.rows) <= end && end <= p.T;
+        }
+        if (!there) {
+            count_error(p, first);
+            return false;
+        }
         w.prefix_chunks = chunk_count(w.prefix, p.prefix_chunk_tokens);
         return true;
     }
@@ -297,7 +309,7 @@ __device__ __forceinline__ bool place_partials(const CacheAttnParams &p, Work &w
     }
     const int after = (w.row0 - row0) * p.group;   // the request's rows lie in its group's
     if ((int64_t)total * p.Hkv > p.prefix_row_blocks || w.prefix_chunks == 0 || after < 0 || after + w.rows > rows) {
-        count_error(p, w.chunk == 0 && w.kvh == 0 && w.row_block == 0);
+        count_error(p, first);
         return false;
     }
     return true;
