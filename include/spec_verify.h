@@ -395,7 +395,8 @@ spec_status spec_kv8_read(const spec_kv8_read_args *args, void *hip_stream);
  * fp32; a token whose softmax weight times V's scale is below 2^-130 of the row's largest such product may be left out of its sums.
  * q is bf16; out is fp32 or bf16.  kv_len[b] may be less than q_len[b] (down to 0): a query row whose position
  * kv_len[b] - q_len[b] + j is negative sees no key, and its output row is zero.  q_len[b] <= SPEC_K_MAX + 1,
- * Hq / Hkv <= 16.
+ * Hq / Hkv <= 16; SPEC_EUNSUPPORTED where the split of one request's tokens would leave more than 4 GiB of partial results (contexts
+ * of millions of tokens).
  */
 typedef struct {
     int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;

@@ -386,6 +386,8 @@ spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t wor
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
     if (a->B > 65535 || (!pl.prefix_many_rows && pl.prefix_row_blocks > 65535) || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
     if (pl.blocks > kMaxPacked || pl.prefix_blocks > (pl.prefix_many_rows ? kMaxPrefixBlocks : kMaxPacked)) return SPEC_EUNSUPPORTED;
+    // (a request's partial results are addressed with 32-bit offsets)
+    if (pl.max_chunks > 1 && (int64_t)pl.max_q_rows * a->Hkv * pl.max_chunks * a->d * 4 > UINT32_MAX) return SPEC_EUNSUPPORTED;
     char *ws = static_cast<char *>(workspace);
     CacheAttnParams p;
     memset(&p, 0, sizeof p);
