@@ -46,9 +46,10 @@ bool prefix_sum_ok(const int32_t *cu, int n, int total)
 spec_status check_append(const spec_kv8_append_args *a)
 {
     if (a == nullptr || a->B < 1 || a->Hkv < 1 || a->T < 0 || a->num_blocks < 1 || a->max_blocks_per_req < 1) return SPEC_EINVAL;
-    if (a->new_k == nullptr || a->new_v == nullptr || a->k_cache == nullptr || a->v_cache == nullptr || a->kv_scale == nullptr ||
-        a->block_table == nullptr || a->kv_len == nullptr || a->cu_q_len == nullptr || a->host_cu_q_len == nullptr)
+    if (a->k_cache == nullptr || a->v_cache == nullptr || a->kv_scale == nullptr || a->block_table == nullptr || a->kv_len == nullptr ||
+        a->cu_q_len == nullptr || a->host_cu_q_len == nullptr)
         return SPEC_EINVAL;
+    if (a->T > 0 && (a->new_k == nullptr || a->new_v == nullptr)) return SPEC_EINVAL;   // (no rows need no address)
     if (a->src_dtype != SPEC_F32 && a->src_dtype != SPEC_BF16) return SPEC_EINVAL;
     if (a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8) return SPEC_EINVAL;
     if (!aligned(a->k_cache, 32) || !aligned(a->v_cache, 32) || !aligned(a->kv_scale, 32) || !aligned(a->new_k, 16) || !aligned(a->new_v, 16))
@@ -70,8 +71,9 @@ spec_status check_read(const spec_kv8_read_args *a)
 {
     if (a == nullptr || a->B < 1 || a->Hkv < 1 || a->T < 0 || a->num_blocks < 1 || a->max_blocks_per_req < 1) return SPEC_EINVAL;
     if (a->k_cache == nullptr || a->v_cache == nullptr || a->kv_scale == nullptr || a->block_table == nullptr || a->cu_len == nullptr ||
-        a->host_cu_len == nullptr || a->out_k == nullptr || a->out_v == nullptr)
+        a->host_cu_len == nullptr)
         return SPEC_EINVAL;
+    if (a->T > 0 && (a->out_k == nullptr || a->out_v == nullptr)) return SPEC_EINVAL;
     if (a->kv_dtype != SPEC_E4M3 && a->kv_dtype != SPEC_INT8) return SPEC_EINVAL;
     if (a->out_dtype != SPEC_F32 && a->out_dtype != SPEC_BF16) return SPEC_EINVAL;
     if (!aligned(a->k_cache, 32) || !aligned(a->v_cache, 32) || !aligned(a->kv_scale, 32) || !aligned(a->out_k, 32) || !aligned(a->out_v, 32))

@@ -93,3 +93,19 @@ def test_tensors_of_another_device_are_refused(which):
         x = _pools()[2] if name == "scale" else torch.zeros((5, 2, 64))
         with pytest.raises(ValueError):
             _all(which, **{name: x.to("meta")})
+
+
+def test_an_append_and_a_read_of_no_rows_do_nothing():
+    """An empty tensor has no address."""
+    empty = torch.zeros((0, 2, 64))
+    args, keep = _append(empty)
+    assert args.new_k is None
+    sv.spec_kv8_append(args, stream=_NoStream())
+    k, v, scale = _pools()
+    args, keep = sv.make_kv8_read_args(empty, empty, k, v, scale, torch.zeros((1, 2), dtype=torch.int32), None, _i32(0, 0), [0, 0])
+    assert args.out_k is None
+    sv.spec_kv8_read(args, stream=_NoStream())
+
+
+class _NoStream:
+    cuda_stream = 0
