@@ -210,7 +210,8 @@ def _stream_handle(stream) -> Optional[int]:
     if _raw_stream is None:
         import torch
         torch.cuda.current_stream()   # (initialises the GPU if nothing has)
-        _raw_stream = lambda get=torch._C._cuda_getCurrentRawStream, device=torch.cuda.current_device: get(device())
+        get = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (a private name: without it, the object)
+        _raw_stream = (lambda: get(torch.cuda.current_device())) if get is not None else (lambda: torch.cuda.current_stream().cuda_stream)
     return _raw_stream() or None
 
 
