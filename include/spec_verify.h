@@ -341,6 +341,12 @@ spec_status spec_kv_repack_mfma(const void *src_k, const void *src_v, void *dst_
  * Slots that hold no visible token may hold anything; a visible token's codes are what spec_kv8_append writes
  * (the SPEC_E4M3 codes for NaN, 0x7F and 0xFF, are never among them).
  *
+ * Workspaces of the two attention calls below: as spec_verify_workspace_bytes says of them.  Where a call's own size is not there, a smaller
+ * one may still serve (SPEC_EWORKSPACE if not): tokens are then split no further than the kernels need (every 4096), and prefixes have a launch of their own
+ * only if that leaves less.  So a workspace asked for the largest batch (requests, query rows, prefix tokens, tokens after the prefixes)
+ * serves smaller calls with those heads.
+ * spec_verify_plan and spec_profile_begin / _end know the calls above and not the four below.
+ *
  * Limits of the four calls below: d in {64, 128}; pools, scales and outputs 32-byte aligned, other rows 16-byte
  * aligned.  Request slots with no rows (q_len[b] == 0, a padded batch) are allowed everywhere.
  */
@@ -526,7 +532,7 @@ int32_t spec_argmax_goodput(const spec_goodput_args *args, double *goodput_per_k
 
 /*
  * Measurement aid (not part of the step): per-kernel GPU time from HIP events.
- * Between spec_profile_begin and spec_profile_end every kernel the library
+ * Between spec_profile_begin and spec_profile_end every kernel of the step (those below) that the library
  * launches (up to max_launches of them) gets a pair of events: the step kernel
  * carries them itself (they receive the time stamps of the launch's own begin
  * and end), the other kernels are bracketed by two event records on the launch

@@ -188,12 +188,13 @@ constexpr double kSecondBlock = 1.1;
 constexpr double kCachedTokens = 0.5, kFarTokens = 0.7, kNearBytes = 3e6, kWholeBf16 = 1.15, kWholeInt8 = 1.25, kCacheBytesPerUs = 9e6;
 constexpr double kTwoLaunches = 1.1, kLaunchUs = 2.5, kMemoryBytesPerUs = 5.3e6;
 template <typename F>
-Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, double ticket_us, double busy_tokens, F for_each_job)   // for_each_job(f): f(tokens, rows)
+Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, double ticket_us, double busy_tokens, bool least, F for_each_job)   // for_each_job(f): f(tokens, rows)
 {
     const int most = std::min(kMaxChunkTokens, std::max((most_tokens + kPairTokens - 1) / kPairTokens * kPairTokens, kPairTokens));
     const double units = compute_units();
     const int most_tiles = std::min((most_rows + 15) / 16, kMostTiles);
     Split best = {most_tiles, most, 1e30};
+    if (least) return best;   // the fewest chunks
     for (int tiles = most_tiles; tiles >= 1; --tiles) {
         const double token_us = kTokenUs[tiles] * token_factor;
         for (int len = most; len >= kPairTokens; len = len * 3 / 4 / kPairTokens * kPairTokens) {
@@ -221,11 +222,12 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, d
 // partial results to write and to read back.
 constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kWideStepUs = 1.7, kPieceJoinUs = 0.35;
 template <typename F>
-int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, bool wide, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
+int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, bool wide, bool least, double &best_us, F for_each_group)   // for_each_group(f): f(row blocks, steps)
 {
     const double units = compute_units(), slots = wide ? units : 2 * units, busy_us = wide ? kWideStepUs : kSharedStepUs, factor = d / 128.0 * (codes ? (full ? 1.5 : 1.0) : (full ? 2.0 : 1.45));   // (more terms: more products with V)
     int best = std::min(most_steps, kMaxPrefixSteps);
     best_us = 1e30;
+    if (least) return best;   // the fewest pieces
     for (int len = best; len >= 1; len = std::min(len - 1, len * 7 / 8)) {
         double count = 0.0, sum = 0.0, longest = 0.0, pieces = 0.0;
         for_each_group([&](int64_t row_blocks, int steps) {
@@ -248,7 +250,8 @@ int prefix_piece_steps(int most_steps, int Hkv, int d, bool full, bool codes, bo
     return best;
 }
 
-Plan make_plan(const spec_prefix_attn_args *a)
+// The plan that the models above find the fastest, or the one that leaves the least in the workspace.
+Plan make_plan(const spec_prefix_attn_args *a, bool least)
 {
     Plan pl;
     memset(&pl, 0, sizeof pl);
@@ -273,12 +276,21 @@ Plan make_plan(const spec_prefix_attn_args *a)
     pl.max_q_rows = max_rows;
     pl.capacity = a->max_kv_len > 0 ? a->max_kv_len : max_len;
     auto split_own = [&](int most_tokens, bool whole, double busy_tokens) {
-        return split_jobs(max_rows, most_tokens, a->Hkv, token_factor, kTicketUs, busy_tokens, [&](auto job) {
+        return split_jobs(max_rows, most_tokens, a->Hkv, token_factor, kTicketUs, busy_tokens, least, [&](auto job) {
             for (int b = 0, g = 0; b < a->B; ++b) {
                 const int q = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b], prefix = whole ? 0 : prefix_of(g, b);
                 if (q > 0) job((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) - prefix, q * group);
             }
         });
+    };
+    const size_t rows = (size_t)a->T * a->Hq;
+    auto chunks_of = [](const Split &split, int tokens) { return std::max((tokens + split.length - 1) / split.length, 1); };
+    auto row_blocks_of = [&](const Split &split) { return (max_rows + 16 * split.tiles - 1) / (16 * split.tiles); };
+    auto partial_bytes = [&](int chunks) { return align_up(rows * chunks * a->d * 4) + align_up(rows * chunks * 8); };
+    auto ticket_bytes = [&](const Split &split) { return (size_t)a->B * a->Hkv * row_blocks_of(split) * 8; };
+    auto own_bytes = [&](const Split &split, int tokens) {
+        const int chunks = chunks_of(split, tokens);
+        return chunks > 1 ? partial_bytes(chunks) + align_up(ticket_bytes(split)) : 0;
     };
     Split own = split_own(max_own, false, 1.0);
     int max_prefix = 0;
@@ -308,7 +320,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
             }
             const bool wide = a->d == 128 && padded[1] <= 1.1 * padded[0];
             pl.prefix_rows_log2 = wide ? 8 : 7;
-            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, pl.prefix_rows_log2 == 8, prefix_us, each_group);
+            pl.prefix_piece_steps = prefix_piece_steps(steps_of(max_prefix), a->Hkv, a->d, full, a->kv_dtype != SPEC_BF16, pl.prefix_rows_log2 == 8, least, prefix_us, each_group);
             each_group([&](int64_t row_blocks, int steps) {
                 pl.prefix_blocks += row_blocks * ((steps + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps) * a->Hkv;
             });
@@ -316,7 +328,7 @@ Plan make_plan(const spec_prefix_attn_args *a)
             pl.prefix_row_blocks = (int)std::min<int64_t>(pl.prefix_blocks, INT32_MAX);
             pl.max_prefix_chunks = (steps_of(max_prefix) + pl.prefix_piece_steps - 1) / pl.prefix_piece_steps;
         } else {
-            const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, token_factor, 0.0, 1.0, [&](auto job) {   // (no ticket: the next launch joins)
+            const Split split = split_jobs((int)most_rows, max_prefix, a->Hkv, token_factor, 0.0, 1.0, least, [&](auto job) {   // (no ticket: the next launch joins)
                 for (int g = 0; g < a->G; ++g)
                     if (a->host_prefix_len[g] > 0) job(a->host_prefix_len[g], rows_of(g));
             });
@@ -341,7 +353,8 @@ Plan make_plan(const spec_prefix_attn_args *a)
         const double whole_us = std::max(whole.us * more, walked_tokens * token_bytes * a->Hkv / kCacheBytesPerUs);
         const double shared_us = std::max((own.us + prefix_us) * kTwoLaunches, prefix_tokens * token_bytes * a->Hkv / kMemoryBytesPerUs) + kLaunchUs;
         const int shared = prefix_shared_switch();
-        if (shared < 0 ? whole_us < shared_us : shared == 0) {
+        const bool whole_wins = least ? own_bytes(whole, max_len) < own_bytes(own, max_own) + partial_bytes(pl.max_prefix_chunks) : whole_us < shared_us;
+        if (shared < 0 ? whole_wins : shared == 0) {
             own = whole;
             max_own = max_len;
             pl.whole_context = 1;
@@ -350,17 +363,16 @@ Plan make_plan(const spec_prefix_attn_args *a)
         }
     }
     pl.row_tiles = own.tiles;
-    pl.row_blocks = (max_rows + 16 * pl.row_tiles - 1) / (16 * pl.row_tiles);
+    pl.row_blocks = row_blocks_of(own);
     pl.chunk_tokens = own.length;
-    pl.max_chunks = std::max((max_own + pl.chunk_tokens - 1) / pl.chunk_tokens, 1);
+    pl.max_chunks = chunks_of(own, max_own);
     pl.blocks = (int64_t)pl.row_blocks * a->B * a->Hkv * pl.max_chunks;
-    const size_t rows = (size_t)a->T * a->Hq;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes); return here; };
     if (pl.max_chunks > 1) {
         pl.acc = take(rows * pl.max_chunks * a->d * 4);
         pl.ml = take(rows * pl.max_chunks * 8);
-        pl.tickets = take((size_t)a->B * a->Hkv * pl.row_blocks * 8);
+        pl.tickets = take(ticket_bytes(own));
     }
     if (pl.max_prefix_chunks > 0) {
         pl.prefix_acc = take(rows * pl.max_prefix_chunks * a->d * 4);
@@ -384,7 +396,8 @@ uint32_t next_generation()
 
 spec_status run_attn(const spec_prefix_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    const Plan pl = make_plan(a);
+    Plan pl = make_plan(a, false);
+    if (workspace_bytes < pl.total) pl = make_plan(a, true);   // (sized for another batch: fewer chunks may still fit)
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < pl.total) return SPEC_EWORKSPACE;
     if (a->B > 65535 || (!pl.prefix_many_rows && pl.prefix_row_blocks > 65535) || pl.row_blocks * pl.max_chunks > 65535) return SPEC_EUNSUPPORTED;   // (grid)
     if (pl.blocks > kMaxPacked || pl.prefix_blocks > (pl.prefix_many_rows ? kMaxPrefixBlocks : kMaxPacked)) return SPEC_EUNSUPPORTED;
@@ -481,7 +494,7 @@ size_t spec_kv8_attn_workspace_bytes(const spec_kv8_attn_args *a)
 {
     if (check_kv8_attn(a) != SPEC_OK) return 0;
     const spec_prefix_attn_args x = as_prefix_args(a);
-    return make_plan(&x).total;
+    return make_plan(&x, false).total;
 }
 
 spec_status spec_kv8_attn(const spec_kv8_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -494,7 +507,7 @@ spec_status spec_kv8_attn(const spec_kv8_attn_args *a, void *workspace, size_t w
 
 size_t spec_prefix_attn_workspace_bytes(const spec_prefix_attn_args *a)
 {
-    return check_prefix_attn(a) == SPEC_OK ? make_plan(a).total : 0;
+    return check_prefix_attn(a) == SPEC_OK ? make_plan(a, false).total : 0;
 }
 
 spec_status spec_prefix_attn(const spec_prefix_attn_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
