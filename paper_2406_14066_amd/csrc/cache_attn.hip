@@ -25,14 +25,15 @@
 
 namespace specv {
 
-// Variants are chosen by (row tiles, head dim, type of the output); one set per kind of cache.
+// Variants are chosen by (row tiles or wavefronts, head dim, type of the output); one set per kind of cache.
 struct CacheLaunch {
     dim3 blocks;
     int prefix;      // which of the two launches
-    int many_rows;   // the prefix's is prefix_rows_kernel's
+    int tiles;       // cache_attn_kernel's row tiles; 0: the launch is prefix_rows_kernel's
+    int waves;       // prefix_rows_kernel's wavefronts
 };
 template <int KIND>
-hipError_t launch_cache_kind(const CacheAttnParams &p, int tiles, bool full, CacheLaunch at, hipStream_t stream);
+hipError_t launch_cache_kind(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream);
 
 #if SPEC_CACHE_PART < 4
 
@@ -1271,46 +1272,48 @@ __global__ __launch_bounds__(W * kWave, 2) void prefix_rows_kernel(CacheAttnPara
     }
 }
 
-template <int KIND, int NT, int D, bool FULL>
-void go(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
+template <int KIND, int D, bool FULL>
+hipError_t go(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
 {
-    if (at.many_rows) {
-        if constexpr (NT == 1 || (NT == 2 && D == 128)) hipLaunchKernelGGL((prefix_rows_kernel<KIND, D, FULL, 4 * NT>), at.blocks, dim3(4 * NT * kWave), 0, stream, p);
-        return;
-    }
-    hipLaunchKernelGGL((cache_attn_kernel<KIND, NT, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p, at.prefix);
+    auto rows = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        hipLaunchKernelGGL((prefix_rows_kernel<KIND, D, FULL, W>), at.blocks, dim3(W * kWave), 0, stream, p);
+        return hipGetLastError();
+    };
+    auto own = [&](auto tiles) {
+        hipLaunchKernelGGL((cache_attn_kernel<KIND, decltype(tiles)::value, D, FULL>), at.blocks, dim3(kThreads), 0, stream, p, at.prefix);
+        return hipGetLastError();
+    };
+    if (at.tiles == 0 && at.waves == 4) return rows(std::integral_constant<int, 4>());
+    if constexpr (D == 128)
+        if (at.tiles == 0 && at.waves == 8) return rows(std::integral_constant<int, 8>());
+    if (at.tiles == 1) return own(std::integral_constant<int, 1>());
+    if (at.tiles == 2) return own(std::integral_constant<int, 2>());
+    if (at.tiles == 3) return own(std::integral_constant<int, 3>());
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 template <int KIND>
-hipError_t launch_cache_kind(const CacheAttnParams &p, int tiles, bool full, CacheLaunch at, hipStream_t stream)
+hipError_t launch_cache_kind(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
 {
-    auto by_dim = [&](auto nt) {
-        constexpr int NT = decltype(nt)::value;
-        if (p.d == 128) { if (full) go<KIND, NT, 128, true>(p, at, stream); else go<KIND, NT, 128, false>(p, at, stream); }
-        else { if (full) go<KIND, NT, 64, true>(p, at, stream); else go<KIND, NT, 64, false>(p, at, stream); }
-    };
-    if (tiles == 1) by_dim(std::integral_constant<int, 1>());
-    else if (tiles == 2) by_dim(std::integral_constant<int, 2>());
-    else if (tiles == 3) by_dim(std::integral_constant<int, 3>());
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (p.d == 128) return p.out_f32 ? go<KIND, 128, true>(p, at, stream) : go<KIND, 128, false>(p, at, stream);
+    return p.out_f32 ? go<KIND, 64, true>(p, at, stream) : go<KIND, 64, false>(p, at, stream);
 }
-template hipError_t launch_cache_kind<SPEC_CACHE_PART>(const CacheAttnParams &p, int tiles, bool full, CacheLaunch at, hipStream_t stream);
+template hipError_t launch_cache_kind<SPEC_CACHE_PART>(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream);
 
 #else   // the launch functions
 
 namespace {
 
-hipError_t launch_kind(const CacheAttnParams &p, int tiles, CacheLaunch at, hipStream_t stream)
+hipError_t launch_kind(const CacheAttnParams &p, CacheLaunch at, hipStream_t stream)
 {
-    const bool full = p.out_f32 != 0;
     switch (p.kind) {
-        case kCacheTiles: return launch_cache_kind<kCacheTiles>(p, tiles, full, at, stream);
-        case kCacheTokens: return launch_cache_kind<kCacheTokens>(p, tiles, full, at, stream);
-        case kCacheE4M3: return launch_cache_kind<kCacheE4M3>(p, tiles, full, at, stream);
-        case kCacheInt8: return launch_cache_kind<kCacheInt8>(p, tiles, full, at, stream);
+        case kCacheTiles: return launch_cache_kind<kCacheTiles>(p, at, stream);
+        case kCacheTokens: return launch_cache_kind<kCacheTokens>(p, at, stream);
+        case kCacheE4M3: return launch_cache_kind<kCacheE4M3>(p, at, stream);
+        case kCacheInt8: return launch_cache_kind<kCacheInt8>(p, at, stream);
     }
     return hipErrorInvalidValue;
 }
@@ -1320,11 +1323,12 @@ hipError_t launch_kind(const CacheAttnParams &p, int tiles, CacheLaunch at, hipS
 hipError_t launch_cache_attn(const CacheAttnParams &p, hipStream_t stream)
 {
     if (p.max_prefix_chunks > 0) {
-        const dim3 blocks = p.prefix_many_rows ? dim3(p.prefix_row_blocks) : dim3(p.Hkv, p.prefix_row_blocks, p.max_prefix_chunks);
-        const hipError_t err = launch_kind(p, p.prefix_many_rows ? p.prefix_rows_log2 - 6 : p.prefix_tiles, CacheLaunch{blocks, 1, p.prefix_many_rows}, stream);
+        const CacheLaunch at = p.prefix_many_rows ? CacheLaunch{dim3(p.prefix_row_blocks), 1, 0, (1 << p.prefix_rows_log2) / kPrefixRows}
+                                                  : CacheLaunch{dim3(p.Hkv, p.prefix_row_blocks, p.max_prefix_chunks), 1, p.prefix_tiles, 0};
+        const hipError_t err = launch_kind(p, at, stream);
         if (err != hipSuccess) return err;
     }
-    return launch_kind(p, p.row_tiles, CacheLaunch{dim3(p.Hkv, p.B, p.row_blocks * p.max_chunks), 0, 0}, stream);
+    return launch_kind(p, CacheLaunch{dim3(p.Hkv, p.B, p.row_blocks * p.max_chunks), 0, p.row_tiles, 0}, stream);
 }
 
 #endif
