@@ -178,9 +178,9 @@ constexpr double kSecondBlock = 1.1;
 
 // A prefix is walked once for all of its group's rows by a launch of its own, whose results the own launch takes in; or each request
 // walks its whole context, which is one launch and reads the prefix again for every request, mostly from the caches.  The second is
-// less work than it seems while prefixes are short or groups small (64/8 heads, bf16 pages: two requests behind 512 tokens 13.1 -> 8.2 us, 64
-// behind 512 tokens 35 -> 18; 32/8 heads, 8-bit, 4 x 16 requests behind 2048 tokens 40 -> 29), the first where they are long
-// and groups large (64/8 heads, 64 requests behind 4096 tokens 69 against 87; 32/8 heads, 2 x 64 behind 8192 123 against 273; 16 x 12
+// less work than it seems while prefixes are short or groups small (64/8 heads, bf16 pages: two requests behind 512 tokens 13.1 -> 8.1 us, 64
+// behind 512 tokens 32 -> 16; 32/8 heads, 8-bit, 4 x 16 requests behind 2048 tokens 37 -> 25), the first where they are long
+// and groups large (64/8 heads, 64 requests behind 4096 tokens 74 against 81; 32/8 heads, 2 x 64 behind 8192 115 against 279; 16 x 12
 // requests without drafts behind 8192 125 against 499).  The model of the second: a token that comes from the caches costs a busy compute
 // unit kCachedTokens of its time alone, kFarTokens of it when the prefixes of a KV head do not fit an XCD's L2 well (kNearBytes) or
 // are bf16, twice the bytes; it was found too low by kWhole*; and the caches give kCacheBytesPerUs.  Of the first: the sum of its launches
@@ -217,8 +217,9 @@ Split split_jobs(int most_rows, int most_tokens, int Hkv, double token_factor, d
 
 // Most steps of a piece of the launch for prefixes with many rows, from a model of it.  A block takes kPieceUs besides its steps; a step
 // takes kStepUs while the block has its compute unit for itself, and kSharedStepUs where two share one, which is what fits: matrix cores and
-// vector units are busy at the same time more often (d = 128, weights in one term; measured behind one prefix of 4096 tokens, 64
-// requests, 64/8 heads, k = 2: 24 steps alone 32 us, 12 and 12 together 22 us; wide: a block of eight wavefronts has the unit, 13 steps 22 us).  More blocks than that take turns.  Each piece of a prefix is
+// vector units are busy at the same time more often (d = 128, weights in one term, bf16 pages without the second one; measured behind one prefix of 4096
+// tokens, 64 requests, 64/8 heads, k = 2: 24 steps alone 32 us, 12 and 12 together 22 us; wide: a block of eight wavefronts has the unit, 13 steps 22 us,
+// and 31 with the second term).  More blocks than that take turns.  Each piece of a prefix is
 // partial results to write and to read back.
 constexpr double kPieceUs = 7.0, kStepUs = 1.35, kSharedStepUs = 1.87, kWideStepUs = 1.7, kPieceJoinUs = 0.35;
 template <typename F>
@@ -311,8 +312,9 @@ Plan make_plan(const spec_prefix_attn_args *a, bool least)
                 for (int g = 0; g < a->G; ++g) group((rows_of(g) + (1 << pl.prefix_rows_log2) - 1) >> pl.prefix_rows_log2, steps_of(a->host_prefix_len[g]));
             };
             // Blocks of eight wavefronts and 256 rows where that does not walk many more absent rows: pages are brought in and converted
-            // half as often (64 requests behind 4096 tokens, 64/8 heads, k = 2, bf16: 38.3 -> 34.4 us; three documents of 6000 ..
-            // 20000 tokens, e4m3: 142 -> 137).  With d = 64 more, smaller blocks are as good (15.7 us against 18.4, 18.0 against 16.5 in the next launch).
+            // half as often (calls with 64 requests behind 4096 tokens, 64/8 heads, k = 2, bf16: 78.1 -> 75.6 us; with three documents of 6000 ..
+            // 20000 tokens, e4m3: 161 -> 156.5).  Near the limit there is little between them (one group behind 6144 tokens, bf16: 1632 rows, 1.08 times
+            // as many, 91.6 -> 86.3; 1104, 1.11, 65.7 -> 65.4; 600, 1.2, 46.3 -> 47.5; 320 behind 2048, 1.33, 22.9 -> 28.0).  With d = 64 more, smaller blocks are as good (15.7 us against 18.4, 18.0 against 16.5 in the next launch).
             double padded[2] = {0.0, 0.0};
             for (int wide = 0; wide < 2; ++wide) {
                 pl.prefix_rows_log2 = 7 + wide;

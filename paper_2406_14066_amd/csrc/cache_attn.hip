@@ -390,7 +390,7 @@ struct RowSum {
 // from memory into a wavefront's registers in operand order, and each part of them asks for the next pair as soon as it has been used.
 //
 // What bounds it: with many blocks the bytes of the cache (256 requests of 256 .. 1024 tokens on 64/8 heads, 8-bit, k = 2: 371 MB in
-// 71 us, 5.2 TB/s); with wide rows the instructions of a step, which are conversions and softmax more than matrix products (4 requests of
+// 72 us, 5.1 TB/s); with wide rows the instructions of a step, which are conversions and softmax more than matrix products (4 requests of
 // 6000 .. 32768 tokens, int8, 36 rows, fp32 output: 58 us, 3.8 TB/s; counters: vector instructions 53% of the wavefronts' cycles, matrix
 // instructions 27%, waits 23%); with few blocks latency (one request of 687 tokens: 6.9 us, of which 3.8 is an empty launch).
 // Hence one wavefront a SIMD with as many registers as that allows, the queries in LDS (NT > 1), descriptors and scales by a
@@ -929,13 +929,16 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnParams
 // Two LDS buffers and one barrier per step; operands are read four reads ahead of the products that take them, and both pairs'
 // scores come before one look at the running maximum, so that the second pair's weights are made under the first one's products.
 //
-// What bounds it: behind one prefix of 4096 tokens, 64 requests, 64/8 heads, k = 2, bf16, the launch takes 34 us.  A block of eight
-// wavefronts on each compute unit walks a step in 1.7 us, 1.26 PFLOP/s over the device (a product of two 8192 x 8192 bf16 matrices reaches
-// 1.31, of 4096 x 4096 1.10), for 22 of them; the rest is the start (finding the group, the table, the first pages: 5), the partial
-// results (2.5) and the launch.  8-bit pages add the conversions and the scales (three prefixes of 6000 .. 20000 tokens, 40 rows a
-// request: 135 us, 0.63 PFLOP/s).  Two blocks of four wavefronts a unit take 38 and 142: they bring in and convert every page twice as
-// often.  64 rows a wavefront would halve the operand reads, but its accumulators go to the second register file and come back for
-// every use of the others (37 -> 54 us); three blocks of four wavefronts with one pair a step do as well as two of these but leave half as
+// What bounds it: behind one prefix of 4096 tokens, 64 requests, 64/8 heads, k = 2, bf16, the launch takes 45 us.  A block of eight
+// wavefronts on each compute unit walks a step in 2.4 us, 1.24 PFLOP/s over the device counting the weights' second term and 0.83 without (a product
+// of two 8192 x 8192 bf16 matrices reaches 1.31, of 4096 x 4096 1.10), for 31 of them; the rest is the start (finding the group, the table, the
+// first pages: 5), the partial results (5) and the launch.  With one term the call took 64 instead of 73, and the error of its bf16 output was
+// 1.35 times what rounding leaves.
+// 8-bit pages add the conversions and the scales (three prefixes of 6000 .. 20000 tokens, 40 rows a request: 132 us for 113 GFLOP, of which 26 are of
+// rows that are not there: groups of 648, 320 and 216 rows in blocks of 256); a second term of their weights, whose first has 11 bits,
+// would take a call with them from 147 to 190.  Two blocks of four wavefronts a unit bring in and convert every page twice as
+// often (calls 78 against 75.6, 161 against 156.5).  64 rows a wavefront would halve the operand reads, but its accumulators go to the second register file
+// and come back for every use of the others; three blocks of four wavefronts with one pair a step do as well as two of these but leave half as
 // many partial results again.
 // ---------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
