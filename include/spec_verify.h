@@ -456,7 +456,9 @@ typedef struct {
     void *out;                    /* [T][Hq][d] */
     const int32_t *host_kv_len;   /* HOST copies (host_kv_len may be NULL if max_kv_len > 0) */
     const int32_t *host_cu_q_len, *host_cu_group, *host_prefix_len;
-    int64_t *error_count;         /* as in spec_kv8_attn_args; a group whose prefix does not fit the launch is left out whole */
+    int64_t *error_count;         /* as in spec_kv8_attn_args; a group whose prefix or row offsets do not fit the launch is left out whole.
+                                     (cu_q_len and cu_group are taken to be the host's: offsets by which groups claim each other's rows
+                                     lead nowhere outside the arrays, but are not all found out.) */
     float softmax_scale;          /* 0 means 1/sqrt(d) */
 } spec_prefix_attn_args;
 size_t spec_prefix_attn_workspace_bytes(const spec_prefix_attn_args *args);   /* 0 if the arguments are malformed */
