@@ -345,7 +345,7 @@ spec_status spec_kv_repack_mfma(const void *src_k, const void *src_v, void *dst_
  * one may still serve (SPEC_EWORKSPACE if not): tokens are then split no further than the kernels need (every 4096), and prefixes have a launch of their own
  * only if that leaves less.  So a workspace asked for the largest batch (requests, query rows, prefix tokens, tokens after the prefixes)
  * serves smaller calls with those heads.
- * spec_verify_plan and spec_profile_begin / _end know the calls above and not the four below.
+ * spec_verify_plan and spec_profile_begin / _end know the calls above and not those below.
  *
  * Limits of the four calls below: d in {64, 128}; pools, scales and outputs 32-byte aligned, other rows 16-byte
  * aligned.  Request slots with no rows (q_len[b] == 0, a padded batch) are allowed everywhere.
@@ -463,6 +463,130 @@ typedef struct {
 } spec_prefix_attn_args;
 size_t spec_prefix_attn_workspace_bytes(const spec_prefix_attn_args *args);   /* 0 if the arguments are malformed */
 spec_status spec_prefix_attn(const spec_prefix_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Prompts and bounded caches.  The four calls below bring a prompt's rows to the cache and answer them, and keep a cache that grows
+ * within bounds: spec_qk_norm_rope makes the rows that spec_kv_append or spec_kv8_append put into the pages, spec_prompt_attn is the
+ * attention of any number of rows per request, spec_kv_weight says which tokens the rows looked at, and spec_kv_evict keeps those.
+ * Limits: d in {64, 128}; pools, scales, weights and outputs 32-byte aligned, other rows 16-byte aligned.  Request slots with no rows
+ * (q_len[b] == 0) are allowed everywhere, and so is a batch of them (T == 0: nothing is launched).
+ */
+
+/*
+ * Root-mean-square norms of every query and key head and the rotation by position, in one pass over the rows:
+ *   y = x / sqrt(mean(x^2) + eps) * weight           (no weight: y = x)
+ *   (y_a, y_b) -> scale * (y_a cos - y_b sin, y_b cos + y_a sin),  angle = positions[t] * inv_freq[i]
+ * for the pairs i < rot_dim / 2 of a head's first rot_dim dims: (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved.
+ * The other dims are y as it is.  Norms and products are fp32 (a row's sum of squares must be within its range), angles are 64-bit
+ * products brought below a turn there; an output is rounded once.
+ * out_q may be q and out_k may be k (same address and stride); apart from that outputs and inputs must not overlap.
+ */
+typedef struct {
+    int32_t T, Hq, Hkv, d;        /* Hq or Hkv may be 0 (rows of one kind only) */
+    int32_t dtype;                /* SPEC_F32 or SPEC_BF16: q, k and the outputs */
+    int32_t weight_dtype;         /* SPEC_F32 or SPEC_BF16: q_weight, k_weight */
+    int32_t rot_dim;              /* a multiple of 16, 0 .. d */
+    int32_t interleaved;
+    int64_t q_stride, k_stride;   /* elements from one token's rows to the next one's (slices of a fused projection); 0: packed */
+    int64_t out_q_stride, out_k_stride;
+    const void *q, *k;            /* T tokens of [Hq][d], of [Hkv][d] */
+    void *out_q, *out_k;
+    const void *q_weight, *k_weight;   /* [d]; NULL: no norm for these heads */
+    const int32_t *positions;     /* [T] */
+    const float *inv_freq;        /* [rot_dim / 2] */
+    float eps;                    /* >= 0 */
+    float scale;                  /* of the rotated dims; 0 means 1 */
+} spec_qk_norm_rope_args;
+spec_status spec_qk_norm_rope(const spec_qk_norm_rope_args *args, void *hip_stream);
+
+/*
+ * Causal attention of any number of query rows per request over the paged cache: whole prompts (q_len[b] == kv_len[b]), chunks of prompts behind
+ * what is cached already, single tokens.  Row j of request b sits at position kv_len[b] - q_len[b] + j and sees the keys up to it; its own
+ * K and V are in the pages (spec_kv_append, spec_kv8_append).  A row whose position is negative sees no key: its output is zero and its
+ * lse -infinity.  q is bf16, pages are bf16 in either layout or 8-bit codes with their scales.
+ * Softmax weights enter the product with V as fp32 values in as many 16-bit terms as that takes for SPEC_F32 outputs (bf16 pages three, 8-bit pages two), as one term for
+ * SPEC_BF16 outputs (bf16 pages 8 bits, whose error is about a bf16 output's own rounding; 8-bit pages 11 bits).  Sums are not normalised until the end: |V| up to 2^90; scaled
+ * scores up to 2^28.
+ * An infinity or NaN in K or V reaches the rows that see it and no others.
+ */
+typedef struct {
+    int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;
+    int32_t kv_dtype;             /* SPEC_BF16, SPEC_E4M3 or SPEC_INT8 */
+    int32_t kv_layout;            /* SPEC_BF16: spec_kv_layout; 8-bit pools: SPEC_KV_MFMA */
+    int32_t out_dtype;            /* SPEC_F32 or SPEC_BF16 */
+    int32_t max_kv_len;           /* length bucket, as in spec_attn_args */
+    int64_t q_token_stride;       /* elements from one token's query rows to the next one's; 0: Hq * d */
+    const void *q;                /* T tokens of [Hq][d] bf16 */
+    const void *k_cache, *v_cache;
+    const float *kv_scale;        /* 8-bit pools; NULL otherwise */
+    const int32_t *block_table;   /* [B][max_blocks_per_req] */
+    const int32_t *kv_len;        /* [B], INCLUDING the rows' own tokens */
+    const int32_t *cu_q_len;      /* [B+1] */
+    void *out;                    /* [T][Hq][d] */
+    float *lse;                   /* optional [T][Hq]: natural logarithm of the sum of exp(scaled scores) */
+    const int32_t *host_kv_len;   /* HOST copies (host_kv_len may be NULL if max_kv_len > 0) */
+    const int32_t *host_cu_q_len;
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths do not
+                                     fit the launch (their rows are not written), and block-table entries outside
+                                     [0, num_blocks) (such a page reads as zeros) */
+    float softmax_scale;          /* 0 means 1/sqrt(d) */
+} spec_prompt_attn_args;
+size_t spec_prompt_attn_workspace_bytes(const spec_prompt_attn_args *args);   /* 0 if the arguments are malformed */
+/* A workspace smaller than that (256 bytes at least) serves too: tokens are then not split between blocks. */
+spec_status spec_prompt_attn(const spec_prompt_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The attention weight that every cached token gets from the given query rows:
+ *   weight(token t, KV head h) = before + sum over the rows j that see t and the query heads g of h of exp(scale q_jg . k_t - lse_jg)
+ * for all tokens t < kv_len[b], with the rows at the positions kv_len[b] - q_len[b] + j (give a prompt's last rows alone to ask what
+ * those look at).  `before` is weight_in's value for tokens before kv_len[b] - q_len[b] and 0 for the rows' own tokens, or where weight_in is NULL.
+ * Rows whose lse is not finite count nothing.  The weights of requests without rows stay as they are.  Sums are fp32, in an order that depends on the lengths alone.
+ */
+typedef struct {
+    int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;
+    int32_t kv_dtype, kv_layout, max_kv_len;   /* as in spec_prompt_attn_args */
+    int64_t q_token_stride;
+    const void *q;                /* T tokens of [Hq][d] bf16 */
+    const float *lse;             /* [T][Hq], of the same scores (spec_prompt_attn's) */
+    const void *k_cache;
+    const float *kv_scale;        /* 8-bit pools; NULL otherwise */
+    const int32_t *block_table, *kv_len, *cu_q_len;
+    const float *weight_in;       /* optional, [num_blocks][Hkv][16]; may be `weight` */
+    float *weight;                /* [num_blocks][Hkv][16], by page as the cache; slots that hold no token of these requests stay as they are */
+    const int32_t *host_kv_len, *host_cu_q_len;
+    int64_t *error_count;         /* as in spec_prompt_attn_args (tokens of pages outside the pool have no weight) */
+    float softmax_scale;
+} spec_kv_weight_args;
+spec_status spec_kv_weight(const spec_kv_weight_args *args, void *hip_stream);
+
+/*
+ * Eviction: of request b's kv_len[b] tokens min(kv_len[b], keep[b]) are copied, in their order, into the pages of dst_block_table's row b.
+ * Kept are the first min(first, keep) tokens, the last min(recent, keep - first) and, of those between, the ones with the largest score; the
+ * score is the sum of the token's weights over the KV heads, in 64 bits and rounded to fp32; equal scores: the earlier token; a NaN and a page outside
+ * the pool score below everything.  K, V, scales (8-bit pools) and weights go with the token.  The source pages stay as they are; the destination pages
+ * must not be among the pages that any request of the call reads.
+ */
+typedef struct {
+    int32_t B, Hkv, d, num_blocks, max_blocks_per_req;
+    int32_t kv_dtype;             /* SPEC_F32 (token-major), SPEC_BF16, SPEC_E4M3 or SPEC_INT8 */
+    int32_t kv_layout, max_kv_len;
+    int32_t dst_max_blocks;       /* row length of dst_block_table: keep[b] <= 16 * dst_max_blocks where that many tokens are kept */
+    int32_t first, recent;        /* >= 0 */
+    void *k_cache, *v_cache;
+    float *kv_scale;              /* 8-bit pools; NULL otherwise */
+    float *weight;                /* [num_blocks][Hkv][16] */
+    const int32_t *block_table;   /* [B][max_blocks_per_req] */
+    const int32_t *kv_len;        /* [B] */
+    const int32_t *keep;          /* [B] >= 0 */
+    const int32_t *dst_block_table;   /* [B][dst_max_blocks] */
+    int32_t *new_kv_len;          /* [B] out: tokens kept; -1 for a request that is left out */
+    int32_t *kept;                /* optional out [B][16 * dst_max_blocks]: the kept tokens' indices in ascending order, then -1 */
+    const int32_t *host_kv_len;   /* HOST copy (may be NULL if max_kv_len > 0) */
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths do not fit the tables or the launch, and
+                                     kept tokens of source pages outside the pool (copied as zeros) or for destination pages outside it (not copied) */
+} spec_kv_evict_args;
+size_t spec_kv_evict_workspace_bytes(const spec_kv_evict_args *args);   /* 0 if the arguments are malformed */
+spec_status spec_kv_evict(const spec_kv_evict_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Host-side speculation control (Section 4.1, "Using Goodput for Speculation"; no GPU

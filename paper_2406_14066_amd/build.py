@@ -30,6 +30,9 @@ STEP_PARTS = 5
 # cache_attn.hip: once per kind of cache, and its launch functions (SPEC_CACHE_PART)
 CACHE_KERNEL = "cache_attn.hip"
 CACHE_PARTS = 5
+# prompt_attn.hip: likewise (SPEC_PROMPT_PART)
+PROMPT_KERNEL = "prompt_attn.hip"
+PROMPT_PARTS = 5
 
 
 def compile_jobs(objdir: str):
@@ -41,7 +44,8 @@ def compile_jobs(objdir: str):
     for src in sources():
         stem = os.path.splitext(os.path.basename(src))[0]
         name, parts = {STEP_KERNEL: ("SPEC_STEP_PART", STEP_PARTS),
-                       CACHE_KERNEL: ("SPEC_CACHE_PART", CACHE_PARTS)}.get(os.path.basename(src), (None, 0))
+                       CACHE_KERNEL: ("SPEC_CACHE_PART", CACHE_PARTS),
+                       PROMPT_KERNEL: ("SPEC_PROMPT_PART", PROMPT_PARTS)}.get(os.path.basename(src), (None, 0))
         if parts:
             for part in range(parts):
                 obj = os.path.join(objdir, "%s_part%d.o" % (stem, part))

@@ -96,6 +96,34 @@ class PrefixAttnArgs(C.Structure):
         ("softmax_scale", C.c_float)]
 
 
+class QkNormRopeArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "Hq", "Hkv", "d", "dtype", "weight_dtype", "rot_dim", "interleaved")] + [
+        (n, C.c_int64) for n in ("q_stride", "k_stride", "out_q_stride", "out_k_stride")] + [
+        (n, C.c_void_p) for n in ("q", "k", "out_q", "out_k", "q_weight", "k_weight", "positions", "inv_freq")] + [
+        ("eps", C.c_float), ("scale", C.c_float)]
+
+
+class PromptAttnArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "kv_dtype", "kv_layout", "out_dtype",
+                                         "max_kv_len")] + [("q_token_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "k_cache", "v_cache", "kv_scale", "block_table", "kv_len", "cu_q_len", "out", "lse", "host_kv_len",
+                                  "host_cu_q_len", "error_count")] + [("softmax_scale", C.c_float)]
+
+
+class KvWeightArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "d", "num_blocks", "max_blocks_per_req", "T", "kv_dtype", "kv_layout", "max_kv_len")] + [
+        ("q_token_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q", "lse", "k_cache", "kv_scale", "block_table", "kv_len", "cu_q_len", "weight_in", "weight", "host_kv_len",
+                                  "host_cu_q_len", "error_count")] + [("softmax_scale", C.c_float)]
+
+
+class KvEvictArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hkv", "d", "num_blocks", "max_blocks_per_req", "kv_dtype", "kv_layout", "max_kv_len",
+                                         "dst_max_blocks", "first", "recent")] + [
+        (n, C.c_void_p) for n in ("k_cache", "v_cache", "kv_scale", "weight", "block_table", "kv_len", "keep", "dst_block_table", "new_kv_len",
+                                  "kept", "host_kv_len", "error_count")]
+
+
 class PlanInfo(C.Structure):
     _fields_ = [
         ("attn_path", C.c_int32), ("row_tiles", C.c_int32), ("row_groups", C.c_int32),
@@ -121,6 +149,8 @@ EXPORTS = (
     "spec_acceptance_update", "spec_acceptance_rate", "spec_argmax_goodput",
     "spec_kv8_append", "spec_kv8_read", "spec_kv8_attn", "spec_kv8_attn_workspace_bytes",
     "spec_prefix_attn", "spec_prefix_attn_workspace_bytes",
+    "spec_qk_norm_rope", "spec_prompt_attn", "spec_prompt_attn_workspace_bytes", "spec_kv_weight",
+    "spec_kv_evict", "spec_kv_evict_workspace_bytes",
 )
 NUM_KERNELS = 5
 KERNEL_NAMES = ("step", "attn", "attn_generic", "attn_combine", "reject")
@@ -169,10 +199,12 @@ def lib():
         L.spec_profile_begin.restype = C.c_int
         L.spec_profile_end.argtypes = [C.c_void_p, C.c_void_p]
         L.spec_profile_end.restype = C.c_int
-        for name, args in (("spec_kv8_append", Kv8AppendArgs), ("spec_kv8_read", Kv8ReadArgs)):
+        for name, args in (("spec_kv8_append", Kv8AppendArgs), ("spec_kv8_read", Kv8ReadArgs), ("spec_qk_norm_rope", QkNormRopeArgs),
+                           ("spec_kv_weight", KvWeightArgs)):
             getattr(L, name).argtypes = [C.POINTER(args), C.c_void_p]
             getattr(L, name).restype = C.c_int
-        for name, args in (("spec_kv8_attn", Kv8AttnArgs), ("spec_prefix_attn", PrefixAttnArgs)):
+        for name, args in (("spec_kv8_attn", Kv8AttnArgs), ("spec_prefix_attn", PrefixAttnArgs), ("spec_prompt_attn", PromptAttnArgs),
+                           ("spec_kv_evict", KvEvictArgs)):
             getattr(L, name).argtypes = [C.POINTER(args), C.c_void_p, C.c_size_t, C.c_void_p]
             getattr(L, name).restype = C.c_int
             getattr(L, name + "_workspace_bytes").argtypes = [C.POINTER(args)]
@@ -397,7 +429,7 @@ def _type_of(t, *allowed) -> int:
 
 def _check_tokens(t, like=None):
     """Rows [T, heads, d] whose heads and dims are contiguous; tokens may lie further apart (slices of a fused projection)."""
-    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+    if t.dim() != 3 or (t.numel() > 0 and (t.stride(2) != 1 or t.stride(1) != t.shape[2])):   # (no rows: their strides say nothing)
         raise ValueError("rows must be [T, heads, d] with contiguous heads")
     if like is not None and (t.shape != like.shape or t.dtype != like.dtype or (t.shape[0] > 1 and t.stride(0) != like.stride(0))):
         raise ValueError("rows must agree in shape, dtype and token stride")
@@ -580,6 +612,166 @@ def spec_prefix_attn_workspace_bytes(args: PrefixAttnArgs) -> int:
 def spec_prefix_attn(args: PrefixAttnArgs, workspace, stream=None) -> None:
     _check(lib().spec_prefix_attn(C.byref(args), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                   _stream_handle(stream)), "spec_prefix_attn")
+
+
+# ---------------------------------------------------------------------------
+# Prompts and bounded caches
+# ---------------------------------------------------------------------------
+def make_qk_norm_rope_args(q, k, out_q, out_k, positions, inv_freq, *, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                           scale: float = 1.0):
+    """The argument struct of `spec_qk_norm_rope`: q [T, Hq, d] and k [T, Hkv, d] (float32 or bfloat16; tokens may be strided; either may be
+    None), outputs of the same shapes (or q and k themselves), positions [T] int32, inv_freq [rot_dim / 2] float32, weights [d] or None (no
+    norm).  Returns (args, keepalive)."""
+    import torch
+    a = QkNormRopeArgs()
+    rows = [t for t in (q, k) if t is not None]
+    if not rows:
+        raise ValueError("q or k is needed")
+    like = rows[0]
+    a.T, a.d = like.shape[0], like.shape[2]
+    a.dtype = _type_of(like, SPEC_F32, SPEC_BF16)
+    for t, out in ((q, out_q), (k, out_k)):
+        if (t is None) != (out is None) or (t is not None and (t.shape[0] != a.T or t.shape[2] != a.d or t.dtype != like.dtype or out.shape != t.shape or out.dtype != t.dtype)):
+            raise ValueError("q, k and their outputs must be [T, heads, d] of one dtype")
+    a.Hq, a.Hkv = (0 if t is None else t.shape[1] for t in (q, k))
+    a.q_stride, a.k_stride, a.out_q_stride, a.out_k_stride = (0 if t is None else _check_tokens(t) for t in (q, k, out_q, out_k))
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() < a.T:
+        raise ValueError("positions must be contiguous int32, an entry per token")
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be contiguous float32")
+    weights = [t for t in (q_weight, k_weight) if t is not None]
+    if any(t.dtype != weights[0].dtype or t.numel() != a.d or not t.is_contiguous() for t in weights):
+        raise ValueError("weights must be contiguous [%d] of one dtype" % a.d)
+    a.weight_dtype = _type_of(weights[0], SPEC_F32, SPEC_BF16) if weights else SPEC_F32
+    if any(t is not None and t.device != like.device for t in (q, k, out_q, out_k, positions, inv_freq, q_weight, k_weight)):
+        raise ValueError("all tensors must be on one device")
+    a.rot_dim = 2 * inv_freq.numel()
+    a.interleaved = int(interleaved)
+    a.q, a.k, a.out_q, a.out_k, a.q_weight, a.k_weight = (_dev_ptr(t) for t in (q, k, out_q, out_k, q_weight, k_weight))
+    a.positions, a.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
+    a.eps, a.scale = eps, scale
+    return a, (q, k, out_q, out_k, positions, inv_freq, q_weight, k_weight)
+
+
+def spec_qk_norm_rope(args: QkNormRopeArgs, stream=None) -> None:
+    _check(lib().spec_qk_norm_rope(C.byref(args), _stream_handle(stream)), "spec_qk_norm_rope")
+
+
+def make_prompt_attn_args(q, k_cache, v_cache, block_table, kv_len, cu_q_len, out, host_kv_len, host_cu_q_len, *, lse=None, kv_scale=None,
+                          kv_layout: int = KV_MFMA, softmax_scale: float = 0.0, max_kv_len: int = 0, error_count=None):
+    """The argument struct of `spec_prompt_attn`: q [T, Hq, d] bfloat16 (tokens may be strided; any number of rows per request), bfloat16 pools in
+    either layout or 8-bit pools with kv_scale, out [T, Hq, d] float32 or bfloat16, lse [T, Hq] float32 or None.  Returns (args, keepalive)."""
+    import torch
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    hc = _host_i32(host_cu_q_len)
+    a = PromptAttnArgs()
+    _fill_attn(a, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, hk, hc, softmax_scale, max_kv_len, error_count)
+    a.kv_dtype = _type_of(k_cache, SPEC_BF16, SPEC_E4M3, SPEC_INT8)
+    a.kv_layout = kv_layout
+    _check_lse(lse, q)
+    a.lse = _dev_ptr(lse)
+    return a, (hk, hc, q, k_cache, v_cache, kv_scale, block_table, kv_len, cu_q_len, out, lse, error_count)
+
+
+def _check_lse(lse, q):
+    import torch
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_contiguous() or lse.device != q.device):
+        raise ValueError("lse must be contiguous float32 [T, Hq] on q's device")
+
+
+def spec_prompt_attn_workspace_bytes(args: PromptAttnArgs) -> int:
+    return _workspace_bytes("spec_prompt_attn_workspace_bytes", args)
+
+
+def spec_prompt_attn(args: PromptAttnArgs, workspace, stream=None) -> None:
+    _check(lib().spec_prompt_attn(C.byref(args), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _stream_handle(stream)), "spec_prompt_attn")
+
+
+def alloc_kv_weight(num_blocks: int, Hkv: int, device="cuda"):
+    """The weights of a cache's tokens, by page as the cache."""
+    import torch
+    return torch.zeros((num_blocks, Hkv, BLOCK_SIZE), dtype=torch.float32, device=device)
+
+
+def _check_weight(t, k_cache):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(k_cache.shape[:3]) or not t.is_contiguous() or t.device != k_cache.device):
+        raise ValueError("weights must be contiguous float32 [num_blocks, Hkv, %d] on the pools' device" % BLOCK_SIZE)
+
+
+def make_kv_weight_args(q, lse, k_cache, block_table, kv_len, cu_q_len, weight, host_kv_len, host_cu_q_len, *, weight_in=None, kv_scale=None,
+                        kv_layout: int = KV_MFMA, softmax_scale: float = 0.0, max_kv_len: int = 0, error_count=None):
+    """The argument struct of `spec_kv_weight`: rows q [T, Hq, d] bfloat16 with their lse [T, Hq], the pool of K (with kv_scale if 8-bit), weight
+    [num_blocks, Hkv, 16] float32, and what it adds to (None: nothing; may be `weight`).  Returns (args, keepalive)."""
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    hc = _host_i32(host_cu_q_len)
+    a = KvWeightArgs()
+    a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, k_cache, kv_scale)
+    _type_of(q, SPEC_BF16)
+    a.q_token_stride = _check_tokens(q)
+    a.T, a.Hq = q.shape[:2]
+    if q.shape[2] != a.d or lse is None:
+        raise ValueError("q must be [T, Hq, %d], with its lse" % a.d)
+    _check_lse(lse, q)
+    _check_weight(weight, k_cache)
+    _check_weight(weight_in, k_cache)
+    a.B = hc.shape[0] - 1
+    _check_arrays(k_cache, block_table, hc, hk, error_count, (q, kv_scale), ((kv_len, a.B), (cu_q_len, a.B + 1)))
+    a.max_blocks_per_req = block_table.shape[1]
+    a.kv_dtype = _type_of(k_cache, SPEC_BF16, SPEC_E4M3, SPEC_INT8)
+    a.kv_layout, a.max_kv_len = kv_layout, max_kv_len
+    a.q, a.lse, a.k_cache, a.kv_scale = q.data_ptr(), lse.data_ptr(), k_cache.data_ptr(), _dev_ptr(kv_scale)
+    a.block_table, a.kv_len, a.cu_q_len = block_table.data_ptr(), kv_len.data_ptr(), cu_q_len.data_ptr()
+    a.weight_in, a.weight = _dev_ptr(weight_in), weight.data_ptr()
+    a.host_kv_len = hk.ctypes.data if hk is not None else None
+    a.host_cu_q_len = hc.ctypes.data
+    a.error_count = _dev_ptr(error_count)
+    a.softmax_scale = softmax_scale
+    return a, (hk, hc, q, lse, k_cache, kv_scale, block_table, kv_len, cu_q_len, weight_in, weight, error_count)
+
+
+def spec_kv_weight(args: KvWeightArgs, stream=None) -> None:
+    _check(lib().spec_kv_weight(C.byref(args), _stream_handle(stream)), "spec_kv_weight")
+
+
+def make_kv_evict_args(k_cache, v_cache, weight, block_table, kv_len, keep, dst_block_table, new_kv_len, host_kv_len, *, kept=None, first: int = 0,
+                       recent: int = 0, kv_scale=None, kv_layout: int = KV_MFMA, max_kv_len: int = 0, error_count=None):
+    """The argument struct of `spec_kv_evict`: pools (float32 or bfloat16, or 8-bit with kv_scale) and their tokens' weights, keep [B], the pages
+    that the kept tokens go to, new_kv_len [B] and kept [B, 16 * dst_block_table.shape[1]] (or None).  Returns (args, keepalive)."""
+    import torch
+    hk = _host_i32(host_kv_len) if host_kv_len is not None else None
+    a = KvEvictArgs()
+    a.num_blocks, a.Hkv, a.d = _check_pools(k_cache, v_cache, kv_scale)
+    if weight is None:
+        raise ValueError("weights are needed")
+    _check_weight(weight, k_cache)
+    a.B = block_table.shape[0]
+    if dst_block_table.dim() != 2 or dst_block_table.shape[0] < a.B:
+        raise ValueError("dst_block_table must be [B, n]")
+    a.max_blocks_per_req, a.dst_max_blocks = block_table.shape[1], dst_block_table.shape[1]
+    width = BLOCK_SIZE * a.dst_max_blocks
+    _check_arrays(k_cache, block_table, np.zeros(a.B + 1), hk, error_count, (v_cache, kv_scale),
+                  ((kv_len, a.B), (keep, a.B), (dst_block_table, a.B * a.dst_max_blocks), (new_kv_len, a.B), (kept, a.B * width)))
+    if kept is not None and tuple(kept.shape) != (a.B, width):
+        raise ValueError("kept must be [B, %d]" % width)
+    a.kv_dtype = _type_of(k_cache, SPEC_F32, SPEC_BF16, SPEC_E4M3, SPEC_INT8)
+    a.kv_layout, a.max_kv_len, a.first, a.recent = kv_layout, max_kv_len, first, recent
+    a.k_cache, a.v_cache, a.kv_scale, a.weight = k_cache.data_ptr(), v_cache.data_ptr(), _dev_ptr(kv_scale), weight.data_ptr()
+    a.block_table, a.kv_len, a.keep, a.dst_block_table = block_table.data_ptr(), kv_len.data_ptr(), keep.data_ptr(), dst_block_table.data_ptr()
+    a.new_kv_len, a.kept = new_kv_len.data_ptr(), _dev_ptr(kept)
+    a.host_kv_len = hk.ctypes.data if hk is not None else None
+    a.error_count = _dev_ptr(error_count)
+    return a, (hk, k_cache, v_cache, kv_scale, weight, block_table, kv_len, keep, dst_block_table, new_kv_len, kept, error_count)
+
+
+def spec_kv_evict_workspace_bytes(args: KvEvictArgs) -> int:
+    return _workspace_bytes("spec_kv_evict_workspace_bytes", args)
+
+
+def spec_kv_evict(args: KvEvictArgs, workspace, stream=None) -> None:
+    _check(lib().spec_kv_evict(C.byref(args), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(stream)),
+           "spec_kv_evict")
 
 
 def spec_profile_begin(max_launches: int) -> None:
