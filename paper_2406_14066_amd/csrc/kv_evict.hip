@@ -1,5 +1,5 @@
 // Eviction: a request's tokens with the largest weights, its first and its latest ones go into other pages (spec_kv_evict).
-// Three launches: scores, the choice (a block per request), the copies.
+// Three launches: scores, the choice (a block per request), the copies; short requests' choices make their scores themselves.
 #include "device_util.h"
 #include "prompt_ops.h"
 
@@ -7,7 +7,9 @@ namespace specv {
 
 namespace {
 
-constexpr int kScoreWaves = 4, kChoiceThreads = 1024, kChoiceWaves = kChoiceThreads / kWave, kCopyWaves = 4;
+constexpr int kScoreWaves = 4, kChoiceThreads = kEvictTurn / 4, kChoiceWaves = kChoiceThreads / kWave, kCopyWaves = 4;
+
+constexpr uint32_t kNoScore = 1, kProtected = 0xFFFFFFFFu;   // below and above every score; 0: no token there
 
 // (The library flushes fp32's denormals, and weights may be: their conversions to 64 bits and back are done on the bits.)
 __device__ __forceinline__ double wide(float x)
@@ -17,10 +19,10 @@ __device__ __forceinline__ double wide(float x)
     const double v = (double)(bits & 0x7FFFFFu) * 0x1p-149;
     return bits >> 31 ? -v : v;
 }
-// A score as a word that orders like it, 0 for NaN: the sum rounded to fp32, both zeros alike.
+// A score as a word that orders like it, kNoScore for NaN: the sum rounded to fp32, both zeros alike.
 __device__ __forceinline__ uint32_t ordered(double x)
 {
-    if (!(x == x)) return 0;
+    if (!(x == x)) return kNoScore;
     uint32_t bits;
     if (fabs(x) < 0x1p-126) bits = (uint32_t)rint(fabs(x) * 0x1p149) | (x < 0.0 ? 0x80000000u : 0u);
     else bits = __float_as_uint((float)x);
@@ -44,37 +46,51 @@ __device__ __forceinline__ bool choice_of(const KvEvictParams &p, int b, Choice 
     return true;
 }
 
+__device__ __forceinline__ uint32_t score_of(const KvEvictParams &p, int entry, int slot)
+{
+    if ((unsigned)entry >= (unsigned)p.num_blocks) return kNoScore;
+    const float *from = p.weight + (size_t)entry * p.Hkv * SPEC_BLOCK_SIZE + slot;
+    double sum = 0.0;
+#pragma unroll 8
+    for (int h = 0; h < p.Hkv; ++h) sum += wide(from[h * SPEC_BLOCK_SIZE]);
+    return ordered(sum);
+}
+
+// Where the score of token t is handed over: the choice's threads have 4 * held tokens side by side of each 4096 * held and read them 16 bytes a thread at a time.
+__device__ __forceinline__ int score_place(int t, int held)
+{
+    const int per = 4 * held, all = per * kChoiceThreads, segment = t / all, in = t - segment * all, thread = in / per, e = in - thread * per;
+    return segment * all + (e / 4 * kChoiceThreads + thread) * 4 + e % 4;
+}
+
 // A wavefront takes four pages, a lane a token: the KV heads' weights in order.  Bound by the bytes, and by latency where they are few.
 __global__ __launch_bounds__(kScoreWaves *kWave) void evict_score_kernel(KvEvictParams p)
 {
     const int lane = threadIdx.x % kWave, b = blockIdx.y, t = (blockIdx.x * kScoreWaves + threadIdx.x / kWave) * kWave + lane;
     Choice c;
     if (!choice_of(p, b, c) || t >= c.n || c.n == c.keep) return;
-    const int entry = p.block_table[(size_t)b * p.max_blocks_per_req + t / SPEC_BLOCK_SIZE];
-    uint32_t key = 0;
-    if ((unsigned)entry < (unsigned)p.num_blocks) {
-        const float *from = p.weight + (size_t)entry * p.Hkv * SPEC_BLOCK_SIZE + t % SPEC_BLOCK_SIZE;
-        double sum = 0.0;
-#pragma unroll 8
-        for (int h = 0; h < p.Hkv; ++h) sum += wide(from[h * SPEC_BLOCK_SIZE]);
-        key = ordered(sum);
-    }
-    p.score[(size_t)b * p.score_stride + t] = key;
+    p.score[(size_t)b * p.score_stride + score_place(t, p.held)] = score_of(p, p.block_table[(size_t)b * p.max_blocks_per_req + t / SPEC_BLOCK_SIZE], t % SPEC_BLOCK_SIZE);
 }
 
-// A block per request: the smallest score that stays is found digit by digit (8 bits each, the largest first) from counts; then the
-// tokens are gone through in order, and those that stay find their places from running counts of the scores above and at the smallest
-// one (of which the earliest stay).
+// A block per request: the smallest score that stays is found from counts over 2048 even parts of the interval that it lies in, first that of all
+// scores, then the part in which it was found, and so on (three times at the most); then the tokens that stay find their places from the numbers,
+// before them, of scores above it and at it (of which the earliest stay).  A thread has 4 * HELD tokens side by side; they are in
+// registers throughout, or, longer requests (LONG), fetched again for each pass.  HELD == 1 makes the scores itself.
+// What is handed to the copies is where a token lies: page * 16 + slot, -1 outside the pool.
+// Additions to one counter in LDS go one after another, which is why the parts are even: counts by the scores' leading 8 or 11 bits, which are of
+// a few binary orders, took 44 us for 16 requests of 6000 .. 30000 tokens, votes (no counters, two bits a pass) 76.
+template <int HELD, bool LONG>
 __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictParams p)
 {
-    __shared__ int count[kChoiceWaves][256];
-    __shared__ int total[256];
-    __shared__ uint32_t wave_sum[2][kChoiceWaves];
-    __shared__ uint32_t found_digit;
-    __shared__ int found_rest;
+    constexpr int kBins = 2048, kCopies = 4, kPer = 4 * HELD, kSegment = kPer * kChoiceThreads;
+    __shared__ alignas(16) int count[kCopies][kBins];
+    __shared__ int wave_sum[2][2][kChoiceWaves];
+    __shared__ uint32_t wave_least[kChoiceWaves], wave_most[kChoiceWaves];
+    __shared__ int found_digit, found_rest;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, b = blockIdx.x;
     const int width = p.dst_max_blocks * SPEC_BLOCK_SIZE;
     int32_t *chosen = p.chosen + (size_t)b * width, *kept = p.kept != nullptr ? p.kept + (size_t)b * width : nullptr;
+    const int32_t *table = p.block_table + (size_t)b * p.max_blocks_per_req;
     Choice c;
     const bool ok = choice_of(p, b, c);
     if (tid == 0) {
@@ -84,106 +100,171 @@ __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictPar
     if (kept != nullptr)
         for (int i = (ok ? c.keep : 0) + tid; i < width; i += kChoiceThreads) kept[i] = -1;
     if (!ok) return;
+    auto put = [&](int place, int t, int entry) {
+        chosen[place] = (unsigned)entry < (unsigned)p.num_blocks ? entry * SPEC_BLOCK_SIZE + t % SPEC_BLOCK_SIZE : -1;
+        if (kept != nullptr) kept[place] = t;
+    };
+    if (c.keep == 0) return;
     if (c.keep == c.n) {
-        for (int i = tid; i < c.n; i += kChoiceThreads) {
-            chosen[i] = i;
-            if (kept != nullptr) kept[i] = i;
-        }
+        for (int i = tid; i < c.n; i += kChoiceThreads) put(i, i, table[i / SPEC_BLOCK_SIZE]);
         return;
     }
-    const uint32_t *score = p.score + (size_t)b * p.score_stride;
-    const int lo = c.first, hi = c.n - c.recent;
-    int rest = c.keep - c.first - c.recent;   // of the tokens lo .. hi - 1, fewer than there are
-    uint32_t least = 0;                       // the digits found
+    const uint32_t *score = p.score + (size_t)b * p.score_stride;   // (rows begin at multiples of 16 bytes)
+    const int lo = c.first, hi = c.n - c.recent, segments = LONG ? (c.n + kSegment - 1) / kSegment : 1;
+    uint32_t x[kPer];
+    auto fetch = [&](int segment) {
+        const int i0 = segment * kSegment + tid * kPer;
+        if constexpr (HELD == 1) {
+            const int entry = i0 < c.n ? table[i0 / SPEC_BLOCK_SIZE] : -1;
+            double sum[4] = {0.0, 0.0, 0.0, 0.0};
+            const float *from = p.weight + (size_t)max(entry, 0) * p.Hkv * SPEC_BLOCK_SIZE + i0 % SPEC_BLOCK_SIZE;
+            const bool inside = (unsigned)entry < (unsigned)p.num_blocks;
+            if (inside) {
+#pragma unroll 8
+                for (int h = 0; h < p.Hkv; ++h) {
+                    const f32x4 w = *reinterpret_cast<const f32x4 *>(from + h * SPEC_BLOCK_SIZE);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] += wide(w[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = inside ? ordered(sum[e]) : kNoScore;
+        } else {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(score + segment * kSegment + (k * kChoiceThreads + tid) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = i0 + e >= c.n ? 0 : i0 + e < lo || i0 + e >= hi ? kProtected : x[e];
+    };
+    if (!LONG) fetch(0);
+    int rest = c.keep - c.first - c.recent;   // of the scores in the interval least .. least + span; fewer than there are
+    uint32_t least = kProtected - 1, span = 0;
     if (rest > 0) {
-        for (int digit = 0; digit < 4; ++digit) {
-            const int shift = 24 - 8 * digit;
-            for (int i = tid; i < kChoiceWaves * 256; i += kChoiceThreads) (&count[0][0])[i] = 0;
-            __syncthreads();
-            for (int i = lo + tid; i < hi; i += kChoiceThreads) {
-                const uint32_t s = score[i];
-                if (digit == 0 || s >> (shift + 8) == least) atomicAdd(&count[wave][s >> shift & 255u], 1);
-            }
-            __syncthreads();
-            if (tid < 256) {
-                int sum = 0;
+        uint32_t most = 0;
+        for (int segment = 0; segment < segments; ++segment) {
+            if (LONG) fetch(segment);
 #pragma unroll
-                for (int w = 0; w < kChoiceWaves; ++w) sum += count[w][tid];
-                total[tid] = sum;
+            for (int e = 0; e < kPer; ++e) {
+                least = min(least, x[e] - 1);                        // (no place: 0, which becomes the largest)
+                most = max(most, x[e] == kProtected ? 0u : x[e]);
             }
-            __syncthreads();
-            if (wave == 0) {   // lane l has the digits 255 - 4 l .. 252 - 4 l
-                int mine[4], sum = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum += mine[e] = total[255 - 4 * lane - e];
-                int upto = sum;
-                for (int step = 1; step < kWave; step *= 2) {
-                    const int other = __shfl_up(upto, step);
-                    if (lane >= step) upto += other;
-                }
-                int above = upto - sum;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (above < rest && above + mine[e] >= rest) {
-                        found_digit = 255 - 4 * lane - e;
-                        found_rest = rest - above;
-                    }
-                    above += mine[e];
-                }
-            }
-            __syncthreads();
-            least = least << 8 | found_digit;
-            rest = found_rest;
         }
-    }
-    // scores above `least` stay, and the first `rest` that equal it (none where only protected tokens stay)
-    const bool any = c.keep > c.first + c.recent;
-    int above = 0, equal = 0;    // so far
-    for (int base = 0, turn = 0; base < c.n; base += 4 * kChoiceThreads, turn ^= 1) {
-        const int i0 = base + 4 * tid;
-        uint32_t flags = 0;      // bit e: stays; bit 4 + e: equals
-        uint32_t mine = 0;       // counts: stays << 16 | equals
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = i0 + e;
-            if (i >= c.n) continue;
-            bool stays = i < lo || i >= hi, same = false;
-            if (!stays && any) {
-                const uint32_t s = score[i];
-                stays = s > least;
-                same = s == least;
-            }
-            flags |= (stays ? 1u : 0u) << e | (same ? 16u : 0u) << e;
-            mine += (stays ? 0x10000u : 0u) + (same ? 1u : 0u);
-        }
-        uint32_t upto = mine;
         for (int step = 1; step < kWave; step *= 2) {
-            const uint32_t other = __shfl_up(upto, step);
-            if (lane >= step) upto += other;
+            least = min(least, (uint32_t)__shfl_xor((int)least, step));
+            most = max(most, (uint32_t)__shfl_xor((int)most, step));
         }
-        if (lane == kWave - 1) wave_sum[turn][wave] = upto;
+        if (lane == 0) {
+            wave_least[wave] = least;
+            wave_most[wave] = most;
+        }
         __syncthreads();
-        uint32_t before = upto - mine, all = 0;
 #pragma unroll
         for (int w = 0; w < kChoiceWaves; ++w) {
-            const uint32_t x = wave_sum[turn][w];
-            if (w < wave) before += x;
-            all += x;
+            least = min(least, wave_least[w]);
+            most = max(most, wave_most[w]);
         }
-        int a = above + (int)(before >> 16), q = equal + (int)(before & 0xFFFFu);
+        least += 1;
+        span = most - least;
+#pragma unroll 1
+        for (;;) {
+            const int shift = max(21 - (span != 0 ? __builtin_clz(span) : 32), 0);   // span >> shift < 2048
+            for (int i = tid; i < kCopies * kBins / 4; i += kChoiceThreads) reinterpret_cast<u32x4 *>(&count[0][0])[i] = (u32x4){0, 0, 0, 0};
+            __syncthreads();
+            int *mine_count = count[wave % kCopies];
+            for (int segment = 0; segment < segments; ++segment) {
+                if (LONG) fetch(segment);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool stays = flags >> e & 1u, same = flags >> (4 + e) & 1u;
-            if (stays || (same && q < rest)) {
-                const int place = a + min(q, rest);
-                chosen[place] = i0 + e;
-                if (kept != nullptr) kept[place] = i0 + e;
+                for (int e = 0; e < kPer; ++e)
+                    if (x[e] - least <= span) atomicAdd(&mine_count[(x[e] - least) >> shift], 1);
             }
-            a += stays;
-            q += same;
+            __syncthreads();
+            // thread t has the parts 2047 - 2 t and 2046 - 2 t
+            int mine[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mine[e] = 0;
+#pragma unroll
+                for (int w = 0; w < kCopies; ++w) mine[e] += count[w][kBins - 1 - 2 * tid - e];
+            }
+            int upto = mine[0] + mine[1];
+#pragma unroll
+            for (int step = 1; step < kWave; step *= 2) {
+                const int other = __shfl_up(upto, step);
+                if (lane >= step) upto += other;
+            }
+            if (lane == kWave - 1) wave_sum[0][0][wave] = upto;
+            __syncthreads();
+            int over = upto - mine[0] - mine[1];
+#pragma unroll
+            for (int w = 0; w < kChoiceWaves; ++w)
+                if (w < wave) over += wave_sum[0][0][w];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (over < rest && over + mine[e] >= rest) {
+                    found_digit = kBins - 1 - 2 * tid - e;
+                    found_rest = rest - over;
+                }
+                over += mine[e];
+            }
+            __syncthreads();
+            const uint32_t from = (uint32_t)found_digit << shift;
+            least += from;
+            span = min(span - from, (1u << shift) - 1u);
+            rest = found_rest;
+            if (shift == 0) break;
+            __syncthreads();   // (found_* and the counts have been read)
         }
-        above += (int)(all >> 16);
-        equal += (int)(all & 0xFFFFu);
+    }
+    // scores above `least` stay, and the first `rest` that equal it
+    int above = 0, equal = 0;    // so far
+    for (int segment = 0; segment < segments; ++segment) {
+        if (LONG) fetch(segment);
+        int more = 0, same = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            more += x[e] > least;
+            same += x[e] == least;
+        }
+        int more_upto = more, same_upto = same;
+#pragma unroll
+        for (int step = 1; step < kWave; step *= 2) {
+            const int m = __shfl_up(more_upto, step), q = __shfl_up(same_upto, step);
+            if (lane >= step) {
+                more_upto += m;
+                same_upto += q;
+            }
+        }
+        if (lane == kWave - 1) {
+            wave_sum[segment & 1][0][wave] = more_upto;
+            wave_sum[segment & 1][1][wave] = same_upto;
+        }
+        __syncthreads();
+        int a = above + more_upto - more, q = equal + same_upto - same;
+#pragma unroll
+        for (int w = 0; w < kChoiceWaves; ++w) {
+            const int m = wave_sum[segment & 1][0][w], s = wave_sum[segment & 1][1][w];
+            if (w < wave) {
+                a += m;
+                q += s;
+            }
+            above += m;
+            equal += s;
+        }
+        const int i0 = segment * kSegment + tid * kPer;
+        int entry = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if (e % SPEC_BLOCK_SIZE == 0 && i0 + e < c.n) entry = table[(i0 + e) / SPEC_BLOCK_SIZE];   // (kPer divides a page or is a multiple of it)
+            const bool stays = x[e] > least, ties = x[e] == least;
+            if (stays || (ties && q < rest)) put(a + min(q, rest), i0 + e, entry);
+            a += stays;
+            q += ties;
+        }
     }
 }
 
@@ -196,22 +277,20 @@ __global__ __launch_bounds__(kCopyWaves *kWave) void evict_copy_kernel(KvEvictPa
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kCopyWaves + threadIdx.x / kWave);
     const int index = unit / p.Hkv, kvh = unit - index * p.Hkv;
     if (index >= p.dst_max_blocks) return;
-    const int keep = uniform_load(p.new_kv_len, b), here = min(keep - index * SPEC_BLOCK_SIZE, SPEC_BLOCK_SIZE);
+    // (all asked for before the first is looked at)
+    const int keep = uniform_load(p.new_kv_len, b), to = uniform_load(p.dst_block_table + (size_t)b * p.dst_max_blocks, index);
+    const int place = p.chosen[((size_t)b * p.dst_max_blocks + index) * SPEC_BLOCK_SIZE + s];
+    const int here = min(keep - index * SPEC_BLOCK_SIZE, SPEC_BLOCK_SIZE);
     if (here <= 0) return;
-    const int to = uniform_load(p.dst_block_table + (size_t)b * p.dst_max_blocks, index);
     if ((unsigned)to >= (unsigned)p.num_blocks) {
         if (kvh == 0 && lane == 0 && p.errors != nullptr) atomicAdd(p.errors, (unsigned long long)here);
         return;
     }
     // lane s % 16: where token s comes from
-    int from = -1, slot = 0;
-    if (s < here) {
-        const int t = p.chosen[((size_t)b * p.dst_max_blocks + index) * SPEC_BLOCK_SIZE + s];
-        from = p.block_table[(size_t)b * p.max_blocks_per_req + t / SPEC_BLOCK_SIZE];
-        slot = t % SPEC_BLOCK_SIZE;
-        if ((unsigned)from >= (unsigned)p.num_blocks) from = -1;
-        const unsigned long long bad = __builtin_amdgcn_ballot_w64(from < 0) & 0xFFFFull;
-        if (bad != 0 && kvh == 0 && lane == 0 && p.errors != nullptr) atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad));
+    const int from = s < here && place >= 0 ? place / SPEC_BLOCK_SIZE : -1, slot = place & (SPEC_BLOCK_SIZE - 1);
+    if (kvh == 0 && p.errors != nullptr) {
+        const unsigned long long bad = __builtin_amdgcn_ballot_w64(s < here && from < 0) & 0xFFFFull;
+        if (bad != 0 && lane == 0) atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(bad));
     }
     const int esz = p.kv_dtype == SPEC_F32 ? 4 : p.kv_dtype == SPEC_BF16 ? 2 : 1;
     const bool tiled = p.kv_dtype == SPEC_E4M3 || p.kv_dtype == SPEC_INT8 || p.kv_layout == SPEC_KV_MFMA;
@@ -291,10 +370,17 @@ hipError_t launch_kv_evict(const KvEvictParams &p, hipStream_t stream)
 {
     const unsigned B = (unsigned)p.B;
     constexpr int kScoreTokens = kScoreWaves * kWave;
-    hipLaunchKernelGGL(evict_score_kernel, dim3(p.capacity_tokens / kScoreTokens + 1, B), dim3(kScoreTokens), 0, stream, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(evict_choice_kernel, dim3(B), dim3(kChoiceThreads), 0, stream, p);
+    hipError_t e;
+    // Short requests' choices make their scores: a launch less.  (A block reads the weights of 4096 tokens in about the time that a launch takes.)
+    if (p.held > 1) {
+        hipLaunchKernelGGL(evict_score_kernel, dim3(p.capacity_tokens / kScoreTokens + 1, B), dim3(kScoreTokens), 0, stream, p);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (p.held == 1) hipLaunchKernelGGL((evict_choice_kernel<1, false>), dim3(B), dim3(kChoiceThreads), 0, stream, p);
+    else if (p.held == 4) hipLaunchKernelGGL((evict_choice_kernel<4, false>), dim3(B), dim3(kChoiceThreads), 0, stream, p);
+    else if (p.capacity_tokens <= p.held * kEvictTurn) hipLaunchKernelGGL((evict_choice_kernel<8, false>), dim3(B), dim3(kChoiceThreads), 0, stream, p);
+    else hipLaunchKernelGGL((evict_choice_kernel<8, true>), dim3(B), dim3(kChoiceThreads), 0, stream, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(evict_copy_kernel, dim3((unsigned)(((int64_t)p.dst_max_blocks * p.Hkv + kCopyWaves - 1) / kCopyWaves), B), dim3(kCopyWaves * kWave), 0, stream, p);

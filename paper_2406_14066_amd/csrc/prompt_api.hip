@@ -179,6 +179,8 @@ spec_status check_weight(const spec_kv_weight_args *a)
     return st;
 }
 
+constexpr int kWeightFewWaves = 16;   // wavefronts a compute unit that blocks of several groups of tokens leave at least
+
 spec_status check_evict(const spec_kv_evict_args *a)
 {
     if (a == nullptr || a->B < 1 || a->Hkv < 1 || a->num_blocks < 1 || a->max_blocks_per_req < 1 || a->dst_max_blocks < 1 || a->first < 0 || a->recent < 0)
@@ -199,20 +201,23 @@ spec_status check_evict(const spec_kv_evict_args *a)
             if (a->host_kv_len[b] < 0 || pages_of(a->host_kv_len[b]) > a->max_blocks_per_req || (a->max_kv_len > 0 && a->host_kv_len[b] > a->max_kv_len))
                 return SPEC_EINVAL;
     if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
+    if (a->num_blocks > INT32_MAX / SPEC_BLOCK_SIZE || a->max_blocks_per_req > kMaxPacked / SPEC_BLOCK_SIZE) return SPEC_EUNSUPPORTED;
     if (a->B > kMostGrid || a->Hkv > kMostKvHeads || (int64_t)a->dst_max_blocks * a->Hkv > kMaxPacked || a->dst_max_blocks > kMaxPacked / SPEC_BLOCK_SIZE)
         return SPEC_EUNSUPPORTED;
     return SPEC_OK;
 }
 
 struct EvictPlan {
-    int capacity, score_stride;
+    int capacity, score_stride, held;
     size_t chosen, total;
 };
 EvictPlan plan_evict(const spec_kv_evict_args *a)
 {
     EvictPlan pl;
     pl.capacity = capacity_of(a->B, a->max_kv_len, a->host_kv_len, nullptr);
-    pl.score_stride = (pl.capacity + 3) / 4 * 4;
+    pl.held = pl.capacity <= kEvictTurn ? 1 : pl.capacity <= 4 * kEvictTurn ? 4 : 8;
+    const int64_t segment = (int64_t)pl.held * kEvictTurn;   // (of requests up to kEvictTurn tokens no scores are handed over)
+    pl.score_stride = pl.held == 1 ? 0 : (int)((pl.capacity + segment - 1) / segment * segment);
     pl.chosen = align_up((size_t)a->B * pl.score_stride * 4);
     pl.total = pl.chosen + align_up((size_t)a->B * a->dst_max_blocks * SPEC_BLOCK_SIZE * 4);
     return pl;
@@ -289,6 +294,15 @@ spec_status spec_kv_weight(const spec_kv_weight_args *a, void *hip_stream)
     p.capacity_tokens = capacity_of(a->B, a->max_kv_len, a->host_kv_len, a->host_cu_q_len);
     p.max_tiles = std::max((p.capacity_tokens + kWeightTokens - 1) / kWeightTokens, 1);
     if ((int64_t)p.max_tiles * a->Hkv > kMaxPacked) return SPEC_EUNSUPPORTED;
+    int64_t units = 0;
+    int most_rows = 0;
+    for (int b = 0; b < a->B; ++b) {
+        const int n = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b];
+        most_rows = std::max(most_rows, n * p.group);
+        if (n > 0) units += (int64_t)((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) + kWeightTokens - 1) / kWeightTokens * a->Hkv;
+    }
+    p.form = most_rows <= kWeightFewRows ? kWeightFew : units < 8 * compute_units() ? kWeightShared : kWeightOwn;
+    p.groups = (int)std::min<int64_t>(std::max<int64_t>(units / (kWeightFewWaves * compute_units()), 1), 16);
     p.group_inverse = inverse_of_group(p.group);
     p.scale_log2 = scale_log2_of(a->softmax_scale, a->d);
     p.q_stride = a->q_token_stride != 0 ? a->q_token_stride : (int64_t)a->Hq * a->d;
@@ -310,7 +324,7 @@ spec_status spec_kv_evict(const spec_kv_evict_args *a, void *workspace, size_t w
     memset(&p, 0, sizeof p);
     p.B = a->B; p.Hkv = a->Hkv; p.d = a->d; p.num_blocks = a->num_blocks; p.max_blocks_per_req = a->max_blocks_per_req; p.dst_max_blocks = a->dst_max_blocks;
     p.kv_dtype = a->kv_dtype; p.kv_layout = a->kv_layout; p.first = a->first; p.recent = a->recent;
-    p.capacity_tokens = pl.capacity; p.score_stride = pl.score_stride;
+    p.capacity_tokens = pl.capacity; p.score_stride = pl.score_stride; p.held = pl.held;
     p.k_cache = a->k_cache; p.v_cache = a->v_cache; p.kv_scale = a->kv_scale; p.weight = a->weight;
     p.block_table = a->block_table; p.kv_len = a->kv_len; p.keep = a->keep; p.dst_block_table = a->dst_block_table;
     p.new_kv_len = a->new_kv_len; p.kept = a->kept;

@@ -43,10 +43,18 @@ struct PromptAttnParams {
 __host__ __device__ inline int row_item(int packed, int b, int group, int rows_log2) { return (int)(((int64_t)packed * group) >> rows_log2) + b; }
 hipError_t launch_prompt_attn(const PromptAttnParams &p, hipStream_t stream);
 
-constexpr int kWeightTokens = 64;   // tokens of a block of the weight kernel
+constexpr int kWeightTokens = 32;   // tokens of a wavefront (or block) of the weight kernel
+enum : int32_t {
+    kWeightOwn = 0,      // a block's wavefronts have tokens of their own and go through the same rows
+    kWeightShared = 1,   // ... have the same tokens and share the rows
+    kWeightFew = 2,      // at most kWeightFewRows rows: they stay in LDS, and the wavefronts go through many tokens
+};
+constexpr int kWeightFewRows = 64;
 struct KvWeightParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, kind;
     int32_t d, max_tiles, capacity_tokens;
+    int32_t form;           // one of kWeight*
+    int32_t groups;         // kWeightFew: times 128 tokens that a block takes one after another
     uint32_t group_inverse;
     float scale_log2;
     int32_t reserved;
@@ -59,15 +67,18 @@ struct KvWeightParams {
 };
 hipError_t launch_kv_weight(const KvWeightParams &p, hipStream_t stream);
 
+constexpr int kEvictTurn = 4096;   // tokens of which the choice's threads hold four each
 struct KvEvictParams {
     int32_t B, Hkv, d, num_blocks, max_blocks_per_req, dst_max_blocks;
     int32_t kv_dtype, kv_layout, first, recent, capacity_tokens, score_stride;
+    int32_t held;           // times 4 tokens of a thread of the choice: 1, 4 or 8 (the last for any length)
+    int32_t reserved;
     void *k_cache, *v_cache;
     float *kv_scale, *weight;
     const int32_t *block_table, *kv_len, *keep, *dst_block_table;
     int32_t *new_kv_len, *kept;
     uint32_t *score;        // workspace: [B][score_stride] ordered bits of the scores
-    int32_t *chosen;        // workspace: [B][16 * dst_max_blocks]
+    int32_t *chosen;        // workspace: [B][16 * dst_max_blocks] where the kept tokens lie: page * 16 + slot, -1 outside the pool
     unsigned long long *errors;
 };
 hipError_t launch_kv_evict(const KvEvictParams &p, hipStream_t stream);

@@ -170,7 +170,9 @@ def test_workspaces_depend_on_shapes_and_lengths_alone():
     bucket.host_kv_len = None
     assert L.spec_prompt_attn_workspace_bytes(C.byref(bucket)) > 256
     e = _evict()
-    assert L.spec_kv_evict_workspace_bytes(C.byref(e)) == 512 + 256
+    assert L.spec_kv_evict_workspace_bytes(C.byref(e)) == 256                   # places of 2 x 32 tokens; no scores are handed over
+    e.max_blocks_per_req, e.max_kv_len, e.host_kv_len = 600, 9000, None
+    assert L.spec_kv_evict_workspace_bytes(C.byref(e)) == 2 * 16384 * 4 + 256
 
 
 def test_a_batch_without_rows_is_nothing_to_do():
