@@ -11,7 +11,7 @@ namespace specv {
 
 namespace {
 
-constexpr int kMostGrid = 65535, kMostKvHeads = 65535, kMostChunks = 64;
+constexpr int kMostGrid = 65535, kMostKvHeads = 65535;
 
 bool float_or_bf16(int32_t dtype) { return dtype == SPEC_F32 || dtype == SPEC_BF16; }
 
@@ -98,15 +98,18 @@ spec_status check_prompt(const spec_prompt_attn_args *a)
     return st;
 }
 
-// The launch of the attention, from a model of it in steps of 64 tokens.  A block takes kBlockSteps' worth besides its steps; blocks beyond
-// the ones that the device holds end at different times, which costs half of the longest one; each chunk of a row's tokens is a partial
-// result to write and to read back, kJoinBytesPerStep of which take as long as a step.
+// The launch of the attention, from a model of it in steps of 64 tokens, kStepUs or (256 rows) kWideStepUs each.  A block takes kBlockSteps' worth besides its
+// steps.  Two blocks of four wavefronts fit a compute unit and slow each other down by kTogether; blocks beyond the ones that the device holds end at
+// different times, which costs half of the longest one.  Each chunk of a row's tokens is a partial result to write and to read back; the
+// join is a launch and looks at the chunks in turn.  Measured, us, by chunks of the longest request (planned: *): one token behind 32000, 64/8
+// heads: 8 86, 16 52, 32 38 *, 64 45; 8 requests of 1 .. 9 rows behind 2000 .. 30000: 4 131, 8 104 *, 12 101, 24 109; 512 rows behind 8000: 1 206, 2 140 *, 3 167;
+// a prompt of 4000 tokens: 1 130 *, 2 156, 4 189.
 struct PromptPlan {
     int rows_log2, items, chunk_tokens, max_chunks, capacity;
     size_t acc, ml, total;   // offsets into the workspace
 };
 constexpr int kStep = 64;
-constexpr double kBlockSteps = 3.0, kJoinBytesPerStep = 4e6, kJoinSteps = 3.0;
+constexpr double kStepUs = 1.35, kWideStepUs = 1.7, kBlockSteps = 3.0, kTogether = 1.4, kJoinBytesPerUs = 4e6, kJoinUs = 4.0, kJoinChunkUs = 0.15;
 
 PromptPlan plan_prompt(const spec_prompt_attn_args *a, bool whole)
 {
@@ -120,39 +123,43 @@ PromptPlan plan_prompt(const spec_prompt_attn_args *a, bool whole)
             if (n > 0) request((int64_t)n * group, a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b], n);
         }
     };
-    // Blocks of eight wavefronts and 256 rows where that does not walk many more absent rows: pages are brought in half as often.
+    const int most_steps = std::max((pl.capacity + kStep - 1) / kStep, 1);
+    // Blocks of eight wavefronts and 256 rows, or of four and 128: the first bring pages in half as often, which is the faster the more blocks
+    // there are (a prompt of 4000 tokens, 32/8 heads: 130 against 149 us), unless they walk many more absent rows; the second are done earlier where
+    // there is less than one for each compute unit (1000 tokens: 31 against 27).
     double padded[2] = {0.0, 0.0};
     each_request([&](int64_t rows, int tokens, int) {
         for (int wide = 0; wide < 2; ++wide) padded[wide] += (double)((rows + (128 << wide) - 1) >> (7 + wide) << (7 + wide)) * tokens;
     });
-    const bool wide = a->d == 128 && padded[1] <= 1.1 * padded[0];
-    pl.rows_log2 = wide ? 8 : 7;
-    pl.items = row_item(a->T, a->B, group, pl.rows_log2);
-    const int most_steps = std::max((pl.capacity + kStep - 1) / kStep, 1);
-    const double slots = compute_units() * (wide ? 1.0 : 2.0);
+    const double units = compute_units();
     int best = most_steps;
     double best_cost = 1e300;
-    for (int chunks = 1, last = 0; chunks <= kMostChunks && !whole; chunks = std::max(chunks + 1, chunks * 5 / 4)) {
-        const int length = (most_steps + chunks - 1) / chunks;
-        if (length == last) continue;
-        last = length;
-        double sum = 0.0, count = 0.0, longest = 0.0, bytes = 0.0;
-        each_request([&](int64_t rows, int tokens, int n) {
-            const int64_t blocks = ((rows + (1 << pl.rows_log2) - 1) >> pl.rows_log2) * a->Hkv;
-            const double steps = std::max(tokens - 0.5 * n, 1.0) / kStep, pieces = ceil(steps / length);
-            const double most = std::min((double)length, ceil((double)tokens / kStep));
-            sum += blocks * (steps + pieces * kBlockSteps);
-            count += blocks * pieces;
-            longest = std::max(longest, most + kBlockSteps);
-            if (tokens > length * kStep) bytes += (double)rows * a->Hkv * pieces * a->d * 8.0;
-        });
-        double cost = count <= slots ? longest : std::max(longest, sum / slots + 0.5 * longest);
-        if (bytes > 0.0) cost += kJoinSteps + bytes / kJoinBytesPerStep;
-        if (cost < 0.97 * best_cost) {   // (more chunks only for something)
-            best_cost = cost;
-            best = length;
+    pl.rows_log2 = 7;
+    for (int wide = 0; wide <= (a->d == 128 && padded[1] <= 1.1 * padded[0] ? 1 : 0); ++wide) {
+        const double slots = units * (wide ? 1.0 : 2.0), together = wide ? 1.0 : kTogether;
+        for (int chunks = 1, last = 0; chunks <= (whole ? 1 : kMostPromptChunks); chunks = std::max(chunks + 1, chunks * 5 / 4)) {
+            const int length = (most_steps + chunks - 1) / chunks;
+            if (length == last) continue;
+            last = length;
+            double sum = 0.0, count = 0.0, longest = 0.0, bytes = 0.0;
+            each_request([&](int64_t rows, int tokens, int n) {
+                const int64_t blocks = ((rows + (128 << wide) - 1) >> (7 + wide)) * a->Hkv;
+                const double steps = std::max(tokens - 0.5 * n, 1.0) / kStep, pieces = ceil(steps / length);
+                sum += blocks * (steps + pieces * kBlockSteps);
+                count += blocks * pieces;
+                longest = std::max(longest, std::min((double)length, ceil((double)tokens / kStep)) + kBlockSteps);
+                if (tokens > length * kStep) bytes += (double)rows * a->Hkv * pieces * a->d * 8.0;
+            });
+            double cost = (wide ? kWideStepUs : kStepUs) * (count <= units ? longest : together * (count <= slots ? longest : std::max(longest, sum / slots + 0.5 * longest)));
+            if (bytes > 0.0) cost += kJoinUs + kJoinChunkUs * ceil((double)most_steps / length) + bytes / kJoinBytesPerUs;
+            if (cost < (length == most_steps ? 1.0 : 0.97) * best_cost) {   // (more chunks only for something)
+                best_cost = cost;
+                best = length;
+                pl.rows_log2 = 7 + wide;
+            }
         }
     }
+    pl.items = row_item(a->T, a->B, group, pl.rows_log2);
     pl.chunk_tokens = best * kStep;
     pl.max_chunks = (most_steps + best - 1) / best;
     size_t at = 0;

@@ -525,51 +525,84 @@ hipError_t launch_prompt_kind<SPEC_PROMPT_PART>(const PromptAttnParams &p, hipSt
 
 namespace {
 
-// Joins the partial results of the rows whose tokens are split: a wavefront per row, a lane per chunk, then per D / 64 dims.
+// Joins the partial results of the rows whose tokens are split: four rows a wavefront, 16 lanes and D / 16 dims a lane each.  A lane looks at every
+// 16th chunk's reference and sum; the chunks' factors go round through LDS, and four chunks' results are asked for at a time.  (A
+// wavefront per row took 10 us and more where rows are few, five dependent latencies of which little ran at once.)
 template <int D>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptAttnParams p)
 {
-    constexpr int N = D / kWave;
-    const int lane = threadIdx.x % kWave;
-    const int64_t index = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (index >= (int64_t)p.T * p.Hq) return;
-    const int row = (int)(index / p.Hq), head = (int)(index - (int64_t)row * p.Hq);
+    constexpr int N = D / 16, kRows = 4;
+    __shared__ float factors[4][kRows][kMostPromptChunks];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane / 16, at = lane % 16;
+    const int64_t all = (int64_t)p.T * p.Hq, index = ((int64_t)blockIdx.x * 4 + wave) * kRows + sub;
+    const int row = (int)(min(index, all - 1) / p.Hq), head = (int)(min(index, all - 1) - (int64_t)row * p.Hq);
     const int b = request_of(p.cu_q_len, p.B, row, (int)((int64_t)row * p.B / p.T));
     const int row0 = p.cu_q_len[b], end = p.cu_q_len[b + 1], kv_len = p.kv_len[b];
-    if (row0 < 0 || row < row0 || end <= row || end > p.T || !length_fits(kv_len, p.capacity_tokens, p.max_blocks_per_req)) return;
-    const int q_len = end - row0, past = kv_len - q_len;
-    const int r = (row - row0) * p.group + head % p.group;
-    const int seen = seen_by(past, q_len, q_len * p.group, r >> p.rows_log2 << p.rows_log2, p.rows_log2, p.group, p.group_inverse);
-    const int chunks = chunks_of(seen, p.chunk_tokens);
-    if (chunks == 1 || chunks > p.max_chunks) return;
+    int chunks = 0;
+    if (index < all && row0 >= 0 && row >= row0 && end > row && end <= p.T && length_fits(kv_len, p.capacity_tokens, p.max_blocks_per_req)) {
+        const int r = (row - row0) * p.group + head % p.group;
+        const int seen = seen_by(kv_len - (end - row0), end - row0, (end - row0) * p.group, r >> p.rows_log2 << p.rows_log2, p.rows_log2, p.group, p.group_inverse);
+        chunks = chunks_of(seen, p.chunk_tokens);
+        if (chunks == 1 || chunks > p.max_chunks) chunks = 0;   // (a single chunk's results are in place)
+    }
+    if (__builtin_amdgcn_ballot_w64(chunks > 0) == 0) return;
 
-    f32x2 mine = {-INFINITY, 0.0f};
-    if (lane < chunks) mine = *reinterpret_cast<const f32x2 *>(p.ml + (index * p.max_chunks + lane) * 2);
-    float top = mine.x;
+    constexpr int kEach = kMostPromptChunks / 16;
+    f32x2 mine[kEach];
+    float top = -INFINITY;
 #pragma unroll
-    for (int step = 1; step < kWave; step *= 2) top = fmaxf(top, __shfl_xor(top, step));
-    const float factor = mine.x == -INFINITY ? 0.0f : fast_exp2(mine.x - top);   // (a chunk in which the row sees nothing)
-    float l = mine.x == -INFINITY && mine.y == 0.0f ? 0.0f : mine.y * factor;
-    if (mine.x == -INFINITY && mine.y != 0.0f) l = mine.y;                       // (a NaN)
+    for (int i = 0; i < kEach; ++i) {
+        mine[i] = (f32x2){-INFINITY, 0.0f};
+        if (at + 16 * i < chunks) mine[i] = *reinterpret_cast<const f32x2 *>(p.ml + (index * p.max_chunks + at + 16 * i) * 2);
+        top = fmaxf(top, mine[i].x);
+    }
 #pragma unroll
-    for (int step = 1; step < kWave; step *= 2) l += __shfl_xor(l, step);
-    float sum[N];
+    for (int step = 1; step < 16; step *= 2) top = fmaxf(top, __shfl_xor(top, step));
+    float l = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
-        const float w = __shfl(factor, c);
-        const float *from = p.acc + (index * p.max_chunks + c) * D + lane * N;
-        if (w == 0.0f) continue;
+    for (int i = 0; i < kEach; ++i) {
+        // a chunk in which the row sees nothing, or nothing but scores of -infinity, has no part; one whose sum is NaN has
+        const bool none = mine[i].x == -INFINITY;
+        const float factor = none ? (mine[i].y == 0.0f ? 0.0f : 1.0f) : fast_exp2(mine[i].x - top);
+        l += none ? mine[i].y : mine[i].y * factor;
+        factors[wave][sub][at + 16 * i] = factor;
+    }
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = fmaf(w, from[i], sum[i]);
+    for (int step = 1; step < 16; step *= 2) l += __shfl_xor(l, step);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (chunks == 0) return;
+    f32x4 sum[N / 4];
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) sum[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    const float *from = p.acc + index * p.max_chunks * D + at * 4;
+    constexpr int kAtOnce = 4;
+    for (int c = 0; c < chunks; c += kAtOnce) {
+        f32x4 x[kAtOnce][N / 4];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) x[k][i] = *reinterpret_cast<const f32x4 *>(from + (size_t)min(c + k, chunks - 1) * D + i * 64);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float w = c + k < chunks ? factors[wave][sub][c + k] : 0.0f;
+            if (w != 0.0f) {
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(w, x[k][i][e], sum[i][e]);
+            }
+        }
     }
     const bool b8 = is_8bit(p.kind);
-    const float inv = past + (row - row0) < 0 ? 0.0f : (b8 ? 0x1p22f : 1.0f) / l;
-    if (lane == 0 && p.lse != nullptr) p.lse[index] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(b8 ? l * 0x1p-22f : l)) * kLn2;
+    const float inv = kv_len - end + row < 0 ? 0.0f : (b8 ? 0x1p22f : 1.0f) / l;
+    if (at == 0 && p.lse != nullptr) p.lse[index] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(b8 ? l * 0x1p-22f : l)) * kLn2;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if (p.out_f32) static_cast<float *>(p.out)[index * D + lane * N + i] = sum[i] * inv;
-        else static_cast<__bf16 *>(p.out)[index * D + lane * N + i] = (__bf16)(sum[i] * inv);
+    for (int i = 0; i < N / 4; ++i) {
+        const f32x4 o = sum[i] * inv;
+        if (p.out_f32) *reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + index * D + at * 4 + i * 64) = o;
+        else *reinterpret_cast<u32x2 *>(static_cast<__bf16 *>(p.out) + index * D + at * 4 + i * 64) = __builtin_bit_cast(u32x2, __builtin_convertvector(o, bf16x4));
     }
 }
 
@@ -585,7 +618,7 @@ hipError_t launch_prompt_attn(const PromptAttnParams &p, hipStream_t stream)
     default: e = launch_prompt_kind<kCacheInt8>(p, stream); break;
     }
     if (e != hipSuccess || p.max_chunks == 1) return e;
-    const dim3 grid((unsigned)(((int64_t)p.T * p.Hq + 3) / 4));
+    const dim3 grid((unsigned)(((int64_t)p.T * p.Hq + 15) / 16));
     if (p.d == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((prompt_join_kernel<64>), grid, dim3(256), 0, stream, p);
     return hipGetLastError();

@@ -22,6 +22,8 @@ struct QkNormRopeParams {
 };
 hipError_t launch_qk_norm_rope(const QkNormRopeParams &p, hipStream_t stream);
 
+constexpr int kMostPromptChunks = 64;   // of a row's tokens
+
 // Prompt attention.  The query rows of a request and KV head are counted token by token, the group's heads side by side: row r is head
 // r % group of token r / group.  A block takes 2^rows_log2 of them through a chunk of the tokens they see.  Request b owns the
 // items row_item(cu[b], b) .. row_item(cu[b + 1], b + 1) - 1 of the grid, which are enough for its row blocks; those left over have no work.
