@@ -279,7 +279,7 @@ __global__ __launch_bounds__(W *kWave, 2) void prompt_attn_kernel(PromptAttnPara
     // Operands come from LDS kAhead reads ahead of the products that take them.
     constexpr int kAhead = 4;
     u32x4 operand[kAhead];
-    auto read_k = [&](int buf, int i) { return *reinterpret_cast<const u32x4 *>(sh.k[buf] + i * 1024 + lane * 16); };   // pair i / KS, dims 16 (i % KS) ..
+    auto read_k = [&](int buf, int i) { return *reinterpret_cast<const u32x4 *>(sh.k[buf] + (i % 2 * KS + i / 2) * 1024 + lane * 16); };   // pair i % 2, dims 16 (i / 2) ..
     auto read_v = [&](int buf, int i) {   // page i / SL, dims 32 (i % SL) ..
         if constexpr (TM) {
             const unsigned char *src = sh.v[buf] + (i / SL * SPEC_BLOCK_SIZE + 4 * half + (n16 >> 2)) * v_row_bytes(D) + (i % SL * 32 + 16 * (g & 1) + 4 * (n16 & 3)) * 2;
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(W *kWave, 2) void prompt_attn_kernel(PromptAttnPara
             for (int e = 0; e < 16; ++e) s[h][e] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
-            s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand[i % kAhead]), q[i % KS], s[i / KS], 0, 0, 0);
+            s[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand[i % kAhead]), q[i / 2], s[i % 2], 0, 0, 0);
             if (i + kAhead < 2 * KS) operand[i % kAhead] = read_k(buf, i + kAhead);
         }
     };
