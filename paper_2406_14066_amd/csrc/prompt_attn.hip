@@ -89,7 +89,7 @@ struct PromptShared {
 };
 
 template <int KIND, int D, bool FULL, int W>
-__global__ __launch_bounds__(W *kWave, 2) void prompt_attn_kernel(PromptAttnParams p)
+__global__ __launch_bounds__(W *kWave, D == 64 ? 3 : 2) void prompt_attn_kernel(PromptAttnParams p)
 {
     constexpr int kPerPage = W / kStepPages;             // wavefronts that bring in a page
     constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(W *kWave, 2) void prompt_attn_kernel(PromptAttnPara
     f32x16 s[2];                 // of the step's pairs of pages
     Weights pw[2][2][TERMS];     // ... and their pages
     // Operands come from LDS kAhead reads ahead of the products that take them.
-    constexpr int kAhead = 4;
+    constexpr int kAhead = D == 128 ? 6 : 4;
     u32x4 operand[kAhead];
     auto read_k = [&](int buf, int i) { return *reinterpret_cast<const u32x4 *>(sh.k[buf] + (i % 2 * KS + i / 2) * 1024 + lane * 16); };   // pair i % 2, dims 16 (i / 2) ..
     auto read_v = [&](int buf, int i) {   // page i / SL, dims 32 (i % SL) ..
