@@ -295,8 +295,8 @@ spec_status spec_validate_reject(const spec_reject_args *reject);
  * positions enter the paged cache.  Row cu_q_len[b] + j of new_k / new_v
  * ([T][Hkv][d], same dtype as the cache) is written to token position
  * kv_len[b] - q_len[b] + j of request b, through the block table, in the given
- * page layout.  Everything else in the pools is left as it is.  Device pointers;
- * host_kv_len / host_cu_q_len are HOST copies used for validation only.
+ * page layout, for any number of rows per request from one on (a step's k_b + 1, a prompt).  Everything else in the pools is left as it is.
+ * Device pointers; host_kv_len / host_cu_q_len are HOST copies used for validation only.
  * SPEC_EINVAL if a position falls outside the request's block-table row, or if new_k, new_v or
  * a pool is not 32-byte aligned (rows move as vectors of 8 elements).
  */

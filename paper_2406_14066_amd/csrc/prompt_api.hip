@@ -12,6 +12,8 @@ namespace specv {
 namespace {
 
 constexpr int kMostGrid = 65535, kMostKvHeads = 65535;
+constexpr int64_t kMostThreads = (int64_t)1 << 32;   // of a launch, fewer
+constexpr int64_t kMostSplitRows = (int64_t)1 << 22;   // (token, head) rows whose tokens may be split: the partial results of two chunks are 4 GB
 
 bool float_or_bf16(int32_t dtype) { return dtype == SPEC_F32 || dtype == SPEC_BF16; }
 
@@ -33,7 +35,7 @@ spec_status check_rope(const spec_qk_norm_rope_args *a)
         if (stride[i] != 0 && (stride[i] < (int64_t)(i < 2 ? a->Hq : a->Hkv) * a->d || stride[i] % per != 0)) return SPEC_EINVAL;
     if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
     if (a->rot_dim % 16 != 0) return SPEC_EUNSUPPORTED;
-    if ((int64_t)a->T * ((int64_t)a->Hq + a->Hkv) > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if ((int64_t)a->T * ((int64_t)a->Hq + a->Hkv) > kMaxPacked || a->T > 1 << 25) return SPEC_EUNSUPPORTED;
     return SPEC_OK;
 }
 
@@ -116,6 +118,7 @@ PromptPlan plan_prompt(const spec_prompt_attn_args *a, bool whole)
     PromptPlan pl;
     memset(&pl, 0, sizeof pl);
     const int group = a->Hq / a->Hkv;
+    whole = whole || (int64_t)a->T * a->Hq > kMostSplitRows;
     pl.capacity = capacity_of(a->B, a->max_kv_len, a->host_kv_len, a->host_cu_q_len);
     auto each_request = [&](auto request) {   // (query rows of a KV head, tokens, rows in tokens)
         for (int b = 0; b < a->B; ++b) {
@@ -209,7 +212,7 @@ spec_status check_evict(const spec_kv_evict_args *a)
                 return SPEC_EINVAL;
     if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
     if (a->num_blocks > INT32_MAX / SPEC_BLOCK_SIZE || a->max_blocks_per_req > kMaxPacked / SPEC_BLOCK_SIZE) return SPEC_EUNSUPPORTED;
-    if (a->B > kMostGrid || a->Hkv > kMostKvHeads || (int64_t)a->dst_max_blocks * a->Hkv > kMaxPacked || a->dst_max_blocks > kMaxPacked / SPEC_BLOCK_SIZE)
+    if (a->B > kMostGrid || a->Hkv > kMostKvHeads || (int64_t)a->dst_max_blocks * a->Hkv * 64 >= kMostThreads || a->dst_max_blocks > kMaxPacked / SPEC_BLOCK_SIZE)
         return SPEC_EUNSUPPORTED;
     return SPEC_OK;
 }
@@ -269,7 +272,7 @@ spec_status spec_prompt_attn(const spec_prompt_attn_args *a, void *workspace, si
     if (workspace_bytes < pl.total) pl = plan_prompt(a, true);   // (sized for another call: tokens are not split)
     if (workspace_bytes < pl.total) return SPEC_EWORKSPACE;
     if (a->T == 0) return SPEC_OK;
-    if ((int64_t)pl.items * a->Hkv > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if ((int64_t)pl.items * a->Hkv * (2 << pl.rows_log2) >= kMostThreads) return SPEC_EUNSUPPORTED;   // (two threads a row)
     char *ws = static_cast<char *>(workspace);
     PromptAttnParams p;
     memset(&p, 0, sizeof p);
@@ -300,7 +303,7 @@ spec_status spec_kv_weight(const spec_kv_weight_args *a, void *hip_stream)
     p.d = a->d;
     p.capacity_tokens = capacity_of(a->B, a->max_kv_len, a->host_kv_len, a->host_cu_q_len);
     p.max_tiles = std::max((p.capacity_tokens + kWeightTokens - 1) / kWeightTokens, 1);
-    if ((int64_t)p.max_tiles * a->Hkv > kMaxPacked) return SPEC_EUNSUPPORTED;
+    if ((int64_t)p.max_tiles * a->Hkv * 4 * 64 >= kMostThreads) return SPEC_EUNSUPPORTED;
     int64_t units = 0;
     int most_rows = 0;
     for (int b = 0; b < a->B; ++b) {

@@ -89,7 +89,7 @@ struct PromptShared {
 };
 
 template <int KIND, int D, bool FULL, int W>
-__global__ __launch_bounds__(W *kWave, D == 64 ? 3 : 2) void prompt_attn_kernel(PromptAttnParams p)
+__global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void prompt_attn_kernel(PromptAttnParams p)
 {
     constexpr int kPerPage = W / kStepPages;             // wavefronts that bring in a page
     constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, TM = KIND == kCacheTokens;

@@ -1158,9 +1158,10 @@ spec_status spec_kv_append(const spec_kv_append_args *a, void *hip_stream)
     if (a->host_cu_q_len[0] != 0 || a->host_cu_q_len[a->B] != a->T) return SPEC_EINVAL;
     for (int b = 0; b < a->B; ++b) {
         const int q_len = a->host_cu_q_len[b + 1] - a->host_cu_q_len[b];
-        if (q_len < 1 || q_len > SPEC_K_MAX + 1 || a->host_kv_len[b] < q_len) return SPEC_EINVAL;
+        if (q_len < 1 || a->host_kv_len[b] < q_len) return SPEC_EINVAL;   // (a step's rows, or a prompt's)
         if ((a->host_kv_len[b] + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE > a->max_blocks_per_req) return SPEC_EINVAL;
     }
+    if ((int64_t)a->T * a->Hkv * (a->d / 8) >= (int64_t)1 << 31) return SPEC_EUNSUPPORTED;   // (grid)
     KvAppendParams p;
     memset(&p, 0, sizeof p);
     p.B = a->B; p.Hkv = a->Hkv; p.d = a->d; p.max_blocks_per_req = a->max_blocks_per_req; p.T = a->T;

@@ -95,7 +95,7 @@ E, U = sv.SPEC_EINVAL, sv.SPEC_EUNSUPPORTED
     (_set(rot_dim=-16), E), (_set(interleaved=2), E), (_set(eps=-1e-6), E), (_set(eps=float("nan")), E), (_set(scale=float("inf")), E), (_set(q=None), E),
     (_set(out_k=None), E), (_set(positions=None), E), (_set(inv_freq=None), E), (_set(q=FAKE + 8), E), (_set(out_q=FAKE + 4), E), (_set(k_weight=FAKE + 2), E),
     (_set(q_stride=1023), E), (_set(q_stride=1028), E), (_set(out_k_stride=128), E), (_set(d=96, rot_dim=96), U), (_set(rot_dim=24), U),
-    (_set(T=1 << 30), U),
+    (_set(T=1 << 30), U), (_set(T=(1 << 25) + 1, Hq=1, Hkv=1), U),
 ])
 def test_rope_refuses(mutate, status):
     a = _rope()
