@@ -71,6 +71,23 @@ __device__ __forceinline__ size_t packed_row(const PromptAttnParams &p, int row0
     return (size_t)(row0 + j) * p.Hq + kvh * p.group + (r - j * p.group);
 }
 
+// A block takes 128 or 256 rows of a request and KV head (the group's heads side by side, so that K and V are brought in once for all of them)
+// through a chunk of the tokens they see; row blocks that see most go first.  Its four or eight wavefronts have 32 rows each and walk the
+// same pages, which pass through LDS once for all, a step (64 tokens) at a time, two buffers, one barrier a step.  In LDS the pages lie as the operands of
+// v_mfma_f32_32x32x16 want them, as 16-bit values whatever the cache holds; token-major V by rows, read through the transposing read.
+// (lane = 32 half + c; pair: two of the step's pages)
+//   S^T[token][row] = K[token][:] . Q[row][:]: a pair, 16 dims an instruction, lane (half, c) holds row c, tokens 4 half + 8 i + 0 .. 3
+//   O^T[dim][row] += V^T[dim][token] . P^T[token][row]: a page an instruction, its tokens in that order, so that P goes from one product to the
+//   other without leaving its lane
+// The two pairs' score products take turns (chains on one accumulator wait for themselves: 16384 tokens 3982 -> 3890 us), operands are read six reads ahead.
+//
+// What bounds it: one prompt of 16384 tokens, 64/8 heads, d = 128, bf16: 3.85 ms, 1.14 PFLOP/s of visible pairs (a product of two 8192 x 8192 bf16
+// matrices 1.31).  Matrix cores are busy 55% of the cycles and vector instructions take 40% more; the two wavefronts of a SIMD are in the same phase
+// after each barrier.  The clock is 1.95 GHz under this load and falls further where the phases overlap more (half of the wavefronts half a step
+// behind: as many cycles, 4.0 .. 4.35 ms).  A block takes about 5 us to start and to end, which packed prompts of 700 .. 5000 tokens see ten times a
+// unit (420 us for 389 GFLOP).  Four wavefronts a block bring pages in twice as often (4.27 ms), but are done earlier where there are few.
+// Weights of bf16 outputs are one term: a second one of bf16 pages is half as many products again, for errors of 1.65e-3 instead of 2.1e-3 of the
+// output's norm; those of fp32 outputs three (8-bit pages: two), 2.6e-7.
 template <int KIND, int D, int W>
 struct PromptShared {
     static constexpr int kK = kStepTokens * D * 2;   // of a step
