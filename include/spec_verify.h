@@ -540,7 +540,8 @@ spec_status spec_prompt_attn(const spec_prompt_attn_args *args, void *workspace,
  *   weight(token t, KV head h) = before + sum over the rows j that see t and the query heads g of h of exp(scale q_jg . k_t - lse_jg)
  * for all tokens t < kv_len[b], with the rows at the positions kv_len[b] - q_len[b] + j (give a prompt's last rows alone to ask what
  * those look at).  `before` is weight_in's value for tokens before kv_len[b] - q_len[b] and 0 for the rows' own tokens, or where weight_in is NULL.
- * Rows whose lse is not finite count nothing.  The weights of requests without rows stay as they are.  Sums are fp32, in an order that depends on the lengths alone.
+ * Rows whose lse is not finite count nothing.  The weights of requests without rows stay as they are.  A page's weights are one request's: requests of
+ * a call must not share pages (shared prompts: give them to a request of their own).  Sums are fp32, in an order that depends on the lengths alone.
  */
 typedef struct {
     int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;

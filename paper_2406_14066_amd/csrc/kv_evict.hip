@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kScoreWaves *kWave) void evict_score_kernel(KvEvict
 // registers throughout, or, longer requests (LONG), fetched again for each pass.  HELD == 1 makes the scores itself.
 // What is handed to the copies is where a token lies: page * 16 + slot, -1 outside the pool.
 // Additions to one counter in LDS go one after another, which is why the parts are even: counts by the scores' leading 8 or 11 bits, which are of
-// a few binary orders, took 44 us for 16 requests of 6000 .. 30000 tokens, votes (no counters, two bits a pass) 76.
+// a few binary orders, took 44 us for 16 requests of 8500 .. 30000 tokens, votes (no counters, two bits a pass) 76.
 template <int HELD, bool LONG>
 __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictParams p)
 {
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictPar
 // A wavefront per (page filled, KV head): 16 tokens from wherever they are.  K's 16-byte pieces hold one token each in every layout, so do
 // token-major V's; a tiled V's 16-byte cell holds four tokens, which are picked from their four cells.  Cells that the last page does not fill go out
 // element by element, so that what lies behind the last token stays as it was.
-// Bound by the cache lines that the tokens lie in: 4096 of 6000 .. 30000 tokens of 16 requests, 8 heads, e4m3: 117 us, 77% of the pages' lines in and 138 MB out.
+// Bound by the cache lines that the tokens lie in: 4096 of 8500 .. 30000 tokens of 16 requests, 8 heads, e4m3: 117 us, about four fifths of the pages' lines in and 138 MB out.
 __global__ __launch_bounds__(kCopyWaves *kWave) void evict_copy_kernel(KvEvictParams p)
 {
     const int lane = threadIdx.x % kWave, b = blockIdx.y, s = lane & 15, g = lane >> 4;

@@ -11,7 +11,7 @@ constexpr int kWeightWaves = 4, kTileRows = 32;
 
 // 32 tokens of a request and KV head are a wavefront's, or, where there are too few of them for the device (kWeightShared), a block's, whose
 // wavefronts take the rows in turn.  The query rows that see any of the block's tokens pass through LDS, 64 (shared: 128) at a time, as rows: read from
-// memory in operand order they would be 64 lanes in 64 cache lines each time (32 rows of 4 x 8000 tokens, 64/8 heads: 42 us, with rows in LDS 28).
+// memory in operand order they would be 64 lanes in 64 cache lines each time (32 rows of four requests of 4500 .. 9400 tokens, 64/8 heads: 42 us, with rows in LDS 28).
 // S[row][token] = Q[row][:] . K[token][:] with v_mfma_f32_32x32x16_bf16, K's 32 tokens held in registers: lane (half, c) holds token c,
 // rows 8 i + 4 half .. + 3, so that a token's sum is the lane's own additions, one exchange with the other half, and
 // (shared) four wavefronts through LDS, in a fixed order.

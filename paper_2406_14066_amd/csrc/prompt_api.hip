@@ -57,17 +57,14 @@ spec_status check_rows(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t nu
     if (!(softmax_scale >= 0.0f) || isinf(softmax_scale)) return SPEC_EINVAL;
     if (q_token_stride != 0 && (q_token_stride < (int64_t)Hq * d || q_token_stride % 8 != 0)) return SPEC_EINVAL;
     if (!prefix_sum_ok(host_cu_q_len, B, T)) return SPEC_EINVAL;
-    int most = 0;
     for (int b = 0; b < B; ++b) {
-        const int n = host_cu_q_len[b + 1] - host_cu_q_len[b];
-        most = std::max(most, n);
-        if (host_kv_len == nullptr || n == 0) continue;
+        if (host_kv_len == nullptr || host_cu_q_len[b + 1] == host_cu_q_len[b]) continue;
         const int len = host_kv_len[b];
         if (len < 0 || pages_of(len) > max_blocks_per_req || (max_kv_len > 0 && len > max_kv_len)) return SPEC_EINVAL;
     }
     if (d != 64 && d != 128) return SPEC_EUNSUPPORTED;
     if (Hq / Hkv > 16 || Hkv > kMostKvHeads || B > kMostGrid) return SPEC_EUNSUPPORTED;
-    if ((int64_t)T * Hq > kMaxPacked || (int64_t)most * (Hq / Hkv) >= kMaxHeadRows) return SPEC_EUNSUPPORTED;
+    if ((int64_t)T * Hq > kMaxPacked || (int64_t)T * (Hq / Hkv) >= kMaxHeadRows) return SPEC_EUNSUPPORTED;   // (of T: whatever the offsets in device memory say)
     return SPEC_OK;
 }
 

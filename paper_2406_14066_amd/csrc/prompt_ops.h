@@ -7,7 +7,7 @@ namespace specv {
 
 // r / group for r < 2^28 and group <= 16: a product with a rounded-up reciprocal.
 inline uint32_t inverse_of_group(int group) { return (uint32_t)((((uint64_t)1 << 32) + group - 1) / group); }   // (unused where the group is 1)
-constexpr int64_t kMaxHeadRows = (int64_t)1 << 28;   // query rows of a request and KV head
+constexpr int64_t kMaxHeadRows = (int64_t)1 << 28;   // query rows of a KV head
 __device__ __forceinline__ int divide_by_group(int r, int group, uint32_t inverse) { return group == 1 ? r : (int)__umulhi((uint32_t)r, inverse); }
 
 struct QkNormRopeParams {

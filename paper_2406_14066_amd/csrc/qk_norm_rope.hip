@@ -49,7 +49,7 @@ __device__ __forceinline__ void write_eight(T *to, const float *x)
 // and keys alike, in p.per_wave such passes.  A token's angles are found once per wavefront, one a lane, and handed round: the 64-bit
 // product is brought to within an eighth of a turn of a multiple of a quarter before it becomes fp32, so that far positions are as exact as
 // near ones.
-// Bound by the bytes of the rows (20500 tokens of packed prompts, 72 heads of 128, bf16: 378 MB in 80 us, 4.7 TB/s); a step's few rows by the launch and
+// Bound by the bytes of the rows (10256 tokens of packed prompts, 72 heads of 128, bf16: 378 MB in 80 us, 4.7 TB/s); a step's few rows by the launch and
 // the chain position -> angle -> rows (five rows: 4.6 us).
 template <typename T, int D, bool INTERLEAVED>
 __global__ __launch_bounds__(kBlockWaves *kWave) void qk_norm_rope_kernel(QkNormRopeParams p)

@@ -147,6 +147,19 @@ def test_kv_evict_refuses(mutate, status):
     assert _call(a) == status
 
 
+@pytest.mark.parametrize("make", [_prompt, _weight])
+def test_more_rows_than_a_kv_head_can_have_are_refused(make):
+    """T tokens times the group: 2^28 is one too many, whatever the requests are."""
+    a = make(kv_len=(60, 60), q_len=(1, 1))
+    a.Hq, a.Hkv, a.T = 16, 1, 1 << 24
+    _host("host_cu_q_len", [0, 1 << 23, 1 << 24])(a)
+    assert _call(a) == U
+    a.T -= 1
+    _host("host_cu_q_len", [0, 1 << 23, (1 << 24) - 1])(a)
+    if make is _prompt:
+        assert sv.lib().spec_prompt_attn_workspace_bytes(C.byref(a)) == 256      # (rows like these are not split)
+
+
 def test_null_arguments_and_workspaces():
     L = sv.lib()
     assert L.spec_qk_norm_rope(None, None) == E and L.spec_prompt_attn(None, FAKE, WORKSPACE, None) == E
