@@ -479,7 +479,7 @@ spec_status spec_prefix_attn(const spec_prefix_attn_args *args, void *workspace,
  * for the pairs i < rot_dim / 2 of a head's first rot_dim dims: (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved.
  * The other dims are y as it is.  Norms and products are fp32 (a row's sum of squares must be within its range), angles are 64-bit
  * products brought below a turn there; an output is rounded once.
- * out_q may be q and out_k may be k (same address and stride); apart from that outputs and inputs must not overlap.
+ * out_q may be q and out_k may be k (same address and stride, SPEC_EINVAL otherwise); apart from that outputs and inputs must not overlap.
  */
 typedef struct {
     int32_t T, Hq, Hkv, d;        /* Hq or Hkv may be 0 (rows of one kind only) */
@@ -552,10 +552,11 @@ typedef struct {
     const void *k_cache;
     const float *kv_scale;        /* 8-bit pools; NULL otherwise */
     const int32_t *block_table, *kv_len, *cu_q_len;
-    const float *weight_in;       /* optional, [num_blocks][Hkv][16]; may be `weight` */
+    const float *weight_in;       /* optional, [num_blocks][Hkv][16]; may be `weight`, must not overlap it otherwise */
     float *weight;                /* [num_blocks][Hkv][16], by page as the cache; slots that hold no token of these requests stay as they are */
     const int32_t *host_kv_len, *host_cu_q_len;
-    int64_t *error_count;         /* as in spec_prompt_attn_args (tokens of pages outside the pool have no weight) */
+    int64_t *error_count;         /* as in spec_prompt_attn_args (tokens of pages outside the pool have no weight; requests to which offsets in device
+                                     memory give more rows than host_cu_q_len planned for may be left out, and are counted) */
     float softmax_scale;
 } spec_kv_weight_args;
 spec_status spec_kv_weight(const spec_kv_weight_args *args, void *hip_stream);
@@ -565,7 +566,7 @@ spec_status spec_kv_weight(const spec_kv_weight_args *args, void *hip_stream);
  * Kept are the first min(first, keep) tokens, the last min(recent, keep - first) and, of those between, the ones with the largest score; the
  * score is the sum of the token's weights over the KV heads, in 64 bits and rounded to fp32; equal scores: the earlier token; a NaN and a page outside
  * the pool score below everything.  K, V, scales (8-bit pools) and weights go with the token.  The source pages stay as they are; the destination pages
- * must not be among the pages that any request of the call reads.
+ * must not be among the pages that any request of the call reads, and each is one request's, once.
  */
 typedef struct {
     int32_t B, Hkv, d, num_blocks, max_blocks_per_req;
@@ -580,7 +581,7 @@ typedef struct {
     const int32_t *kv_len;        /* [B] */
     const int32_t *keep;          /* [B] >= 0 */
     const int32_t *dst_block_table;   /* [B][dst_max_blocks] */
-    int32_t *new_kv_len;          /* [B] out: tokens kept; -1 for a request that is left out */
+    int32_t *new_kv_len;          /* [B] out: tokens kept; -1 for a request that is left out.  Must not overlap kv_len or keep */
     int32_t *kept;                /* optional out [B][16 * dst_max_blocks]: the kept tokens' indices in ascending order, then -1 */
     const int32_t *host_kv_len;   /* HOST copy (may be NULL if max_kv_len > 0) */
     int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths do not fit the tables or the launch, and

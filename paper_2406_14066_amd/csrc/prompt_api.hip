@@ -15,6 +15,13 @@ constexpr int kMostGrid = 65535, kMostKvHeads = 65535;
 constexpr int64_t kMostThreads = (int64_t)1 << 32;   // of a launch, fewer
 constexpr int64_t kMostSplitRows = (int64_t)1 << 22;   // (token, head) rows whose tokens may be split: the partial results of two chunks are 4 GB
 
+// Whether two arrays of so many bytes share some.
+bool overlap(const void *a, const void *b, size_t bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return (x < y ? y - x : x - y) < bytes;
+}
+
 bool float_or_bf16(int32_t dtype) { return dtype == SPEC_F32 || dtype == SPEC_BF16; }
 
 spec_status check_rope(const spec_qk_norm_rope_args *a)
@@ -33,6 +40,11 @@ spec_status check_rope(const spec_qk_norm_rope_args *a)
     const int64_t stride[4] = {a->q_stride, a->out_q_stride, a->k_stride, a->out_k_stride};
     for (int i = 0; i < 4; ++i)
         if (stride[i] != 0 && (stride[i] < (int64_t)(i < 2 ? a->Hq : a->Hkv) * a->d || stride[i] % per != 0)) return SPEC_EINVAL;
+    if (a->T > 1) {   // rows that lie on their outputs lie on their own
+        const int64_t q_row = (int64_t)a->Hq * a->d, k_row = (int64_t)a->Hkv * a->d;
+        auto moved = [](const void *from, const void *to, int64_t x, int64_t y, int64_t row) { return from != nullptr && from == to && (x != 0 ? x : row) != (y != 0 ? y : row); };
+        if (moved(a->q, a->out_q, a->q_stride, a->out_q_stride, q_row) || moved(a->k, a->out_k, a->k_stride, a->out_k_stride, k_row)) return SPEC_EINVAL;
+    }
     if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
     if (a->rot_dim % 16 != 0) return SPEC_EUNSUPPORTED;
     if ((int64_t)a->T * ((int64_t)a->Hq + a->Hkv) > kMaxPacked || a->T > 1 << 25) return SPEC_EUNSUPPORTED;
@@ -183,6 +195,7 @@ spec_status check_weight(const spec_kv_weight_args *a)
     if (st == SPEC_EINVAL) return st;
     if (a->weight == nullptr || (a->T > 0 && a->lse == nullptr)) return SPEC_EINVAL;
     if (!aligned(a->weight, 32) || !aligned(a->weight_in, 32) || !aligned(a->lse, 4)) return SPEC_EINVAL;
+    if (a->weight_in != nullptr && a->weight_in != a->weight && overlap(a->weight_in, a->weight, (size_t)a->num_blocks * a->Hkv * SPEC_BLOCK_SIZE * 4)) return SPEC_EINVAL;
     return st;
 }
 
@@ -196,6 +209,8 @@ spec_status check_evict(const spec_kv_evict_args *a)
         a->dst_block_table == nullptr || a->new_kv_len == nullptr)
         return SPEC_EINVAL;
     if (a->dst_block_table == a->block_table) return SPEC_EINVAL;   // (the pages read would be written)
+    for (const int32_t *lengths : {a->kv_len, a->keep})
+        if (overlap(a->new_kv_len, lengths, (size_t)a->B * 4)) return SPEC_EINVAL;   // (a block's wavefronts read them while its first writes)
     const bool b8 = a->kv_dtype == SPEC_E4M3 || a->kv_dtype == SPEC_INT8;
     if (!b8 && !float_or_bf16(a->kv_dtype)) return SPEC_EINVAL;
     if ((a->kv_scale != nullptr) != b8) return SPEC_EINVAL;

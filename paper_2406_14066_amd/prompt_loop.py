@@ -35,6 +35,8 @@ class PromptLoop:
     def __init__(self, requests, prompt, *, budget, chunk=1024, window=32, first=4, recent=64, k=4, steps=12, Hq=32, Hkv=8, d=128, V=4096, kv="bf16",
                  layout=sv.KV_MFMA, sigma=0.773, seed=1, timed=False, device="cuda"):
         import torch
+        if min(requests, prompt[0], chunk, budget, window) < 1 or min(first, recent, k, steps) < 0 or prompt[1] < prompt[0]:
+            raise ValueError("requests, prompts, chunk, budget and window must be positive, first, recent, k and steps not negative")
         self.torch, self.device, self.seed, self.timed = torch, device, seed, timed
         self.B, self.chunk, self.window, self.first, self.recent, self.budget, self.k = requests, chunk, window, first, recent, budget, k
         self.Hq, self.Hkv, self.d, self.V, self.sigma, self.kv, self.layout = Hq, Hkv, d, V, sigma, kv, layout
@@ -204,7 +206,7 @@ def main():
     if not torch.cuda.is_available():
         print("prompt_loop: no GPU visible", file=sys.stderr)
         sys.exit(2)
-    loop = PromptLoop(args.requests, (args.prompt // 2, args.prompt), budget=args.budget, chunk=args.chunk, k=args.k, steps=args.steps, kv=args.kv, timed=True)
+    loop = PromptLoop(args.requests, ((args.prompt + 1) // 2, args.prompt), budget=args.budget, chunk=args.chunk, k=args.k, steps=args.steps, kv=args.kv, timed=True)
     loop.take_prompts()
     loop.evict()
     for _ in range(args.steps):

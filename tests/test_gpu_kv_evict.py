@@ -84,16 +84,17 @@ CASES = [
     ("protected_more_than_kept", [90, 70], [6, 3], 4, 100, 2, 64),
     ("no_protection", [500, 333], [100, 320], 0, 0, 4, 128),
     ("long", [5000, 9000], [1000, 8190], 16, 64, 1, 64),
+]
+LONG_CASES = [   # (lengths concern the choice alone: two kinds of pools)
     ("longer", [20000, 17], [300, 20], 4, 64, 1, 64),
     ("longest", [70001, 40000], [500, 33000], 4, 1000, 1, 64),      # the choice fetches scores again for each pass
 ]
+EACH = [pytest.param(*c, kind, id="%s-%s" % (c[0], kind)) for c in CASES for kind in KINDS]
+EACH += [pytest.param(*c, kind, id="%s-%s" % (c[0], kind)) for c in LONG_CASES for kind in ("tiles", "int8")]
 
 
-@pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("name,kv_len,keep,first,recent,Hkv,d", CASES, ids=[c[0] for c in CASES])
+@pytest.mark.parametrize("name,kv_len,keep,first,recent,Hkv,d,kind", EACH)
 def test_matches_the_definition(name, kv_len, keep, first, recent, Hkv, d, kind):
-    if name.startswith("longe") and kind not in ("tiles", "int8"):
-        pytest.skip("lengths concern the choice alone")
     print("case kv_evict", name, kind, flush=True)
     rng = np.random.default_rng(41)
     (table, new_table), nb = R.tables(rng, kv_len, more=[[min(n, k) for n, k in zip(kv_len, keep)]])
@@ -187,3 +188,49 @@ def test_a_bucket_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         check(state, cache, weight, table, n, keep, new_table, 4, 8)
+
+
+def test_another_stream_and_a_workspace_of_two_graphs():
+    """Two captured calls with one workspace, a choice in one launch and one of scores handed over, replayed in turn; then each on a stream of its own."""
+    import torch
+    rng = np.random.default_rng(46)
+    calls = []
+    for kind, n, keep in (("tiles", 700, 300), ("int8", 6000, 2000)):
+        (table, new_table), nb = R.tables(rng, [n], more=[[keep]])
+        cache = R.Cache(rng, nb, 2, 64, kind)
+        weight = rng.random((nb, 2, 16)).astype(np.float32)
+        calls.append(((cache, weight, table, [n], [keep], new_table, 4, 8),) + tuple(run(cache, weight, table, [n], [keep], new_table, 4, 8, args_only=True)))
+    shared = sv.alloc_workspace(max(sv.spec_kv_evict_workspace_bytes(c[1]) for c in calls))
+    graphs = []
+    for given, args, keepalive, ws, state in calls:
+        sv.spec_kv_evict(args, shared)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sv.spec_kv_evict(args, shared)
+
+    def clear():
+        for given, args, keepalive, ws, state in calls:
+            fresh = given[0].device()
+            for name, new in zip(("k", "v", "scale", "weight"), fresh + (torch.from_numpy(given[1]).cuda(),)):
+                if new is not None:
+                    state[name].view(torch.uint8).copy_(new.view(torch.uint8))
+            state["new_len"].fill_(77)
+            state["kept"].fill_(77)
+        torch.cuda.synchronize()
+
+    def same():
+        torch.cuda.synchronize()
+        for given, args, keepalive, ws, state in calls:
+            check(state, *given)
+
+    for order in ((0, 1), (1, 0), (1, 0)):
+        clear()
+        for i in order:
+            graphs[i].replay()
+        same()
+    clear()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for stream, (given, args, keepalive, ws, state) in zip(streams, calls):
+        sv.spec_kv_evict(args, ws, stream)
+    same()

@@ -137,6 +137,52 @@ def test_findings_and_a_bucket():
     check(got, cache, q, lse, table, [50, 0, 200], cu, None, steep)
 
 
+def test_more_rows_than_planned_are_left_out_and_counted():
+    """Few rows are planned for by the host's offsets; a request to which those in device memory give more than fit is left out."""
+    import torch
+    rng = np.random.default_rng(35)
+    planned, q_len, kv_len, Hq, Hkv, d = [12, 12], [2, 22], [150, 200], 8, 2, 128
+    table, nb = R.tables(rng, kv_len)
+    cache = R.Cache(rng, nb, Hkv, d, "tiles")
+    cu = R.prefix_sum(q_len)
+    q = rng.standard_normal((24, Hq, d))
+    _, lse, _, steep, _ = reference(cache, q, table, kv_len, cu)
+    args, keep, weight, errors = run(cache, q, lse, table, kv_len, R.prefix_sum(planned), args_only=True)
+    device_cu = [t for t in keep if hasattr(t, "is_cuda") and tuple(t.shape) == (3,)][0]
+    device_cu.copy_(_i32(cu))
+    sv.spec_kv_weight(args)
+    torch.cuda.synchronize()
+    got = weight.cpu().numpy()
+    assert (got[table[1]] == 7.0).all() and int(errors.item()) == 1
+    check(got, cache, q[:2], lse[:2], table[:1], kv_len[:1], cu[:2], None, steep[:2])
+
+
+def test_two_calls_at_once():
+    """Two calls on two streams: as one after the other."""
+    import torch
+    rng = np.random.default_rng(36)
+    calls = []
+    for Hq, n in ((8, 9000), (16, 300)):
+        q_len = [40]
+        table, nb = R.tables(rng, [n])
+        cache = R.Cache(rng, nb, 2, 128, "tiles")
+        q, cu = rng.standard_normal((40, Hq, 128)), R.prefix_sum(q_len)
+        lse = reference(cache, q, table, [n], cu)[1]
+        want, _ = run(cache, q, lse, table, [n], cu)
+        calls.append((want,) + tuple(run(cache, q, lse, table, [n], cu, args_only=True)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        for call in calls:
+            call[3].fill_(7.0)
+        torch.cuda.synchronize()
+        for stream, call in zip(streams, calls):
+            sv.spec_kv_weight(call[1], stream)
+        torch.cuda.synchronize()
+        for call in calls:
+            assert (call[3].cpu().numpy() == call[0]).all()
+
+
 def test_a_graph_and_repeats():
     import torch
     rng = np.random.default_rng(34)

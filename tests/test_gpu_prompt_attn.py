@@ -257,6 +257,53 @@ def test_a_bucket_serves_other_lengths_in_a_graph(kind):
     assert int(errors.item()) == 0
 
 
+def test_two_graphs_share_a_workspace_and_two_streams_have_their_own():
+    """Two captured calls with one workspace (both split tokens), replayed in turn on a stream; then both at once, a stream and a workspace each."""
+    import torch
+    rng = np.random.default_rng(23)
+    calls = []
+    for kind, q_len, kv_len, Hq, Hkv, d in (("tiles", [3, 1], [5000, 1234], 8, 1, 128), ("e4m3", [20, 2], [2600, 3000], 4, 2, 64)):
+        table, nb = R.tables(rng, kv_len)
+        cache = R.Cache(rng, nb, Hkv, d, kind)
+        cu = R.prefix_sum(q_len)
+        q = rng.standard_normal((int(cu[-1]), Hq, d))
+        want = run(cache, q, table, kv_len, cu, "f32")
+        assert want[2] == 0
+        calls.append((want,) + tuple(run(cache, q, table, kv_len, cu, "f32", args_only=True)))
+    shared = sv.alloc_workspace(max(sv.spec_prompt_attn_workspace_bytes(c[1]) for c in calls))
+    assert shared.numel() > 256
+    graphs = []
+    for _, args, keep, ws, out, lse, errors in calls:
+        sv.spec_prompt_attn(args, shared)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sv.spec_prompt_attn(args, shared)
+
+    def clear():
+        for c in calls:
+            c[4].fill_(7.0)
+            c[5].fill_(7.0)
+
+    def same():
+        torch.cuda.synchronize()
+        for want, args, keep, ws, out, lse, errors in calls:
+            assert (out.cpu().numpy() == want[0]).all() and (lse.cpu().numpy() == want[1]).all() and int(errors.item()) == 0
+
+    for order in ((0, 1), (1, 0), (0, 1)):
+        clear()
+        for i in order:
+            graphs[i].replay()
+        same()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        clear()
+        torch.cuda.synchronize()
+        for stream, (want, args, keep, ws, out, lse, errors) in zip(streams, calls):
+            sv.spec_prompt_attn(args, ws, stream)
+        same()
+
+
 def test_requests_that_do_not_fit_are_left_out_and_counted():
     import torch
     rng = np.random.default_rng(17)

@@ -54,8 +54,8 @@ def _evict():
     hk = np.array([60, 50], dtype=np.int32)
     a.B, a.Hkv, a.d, a.num_blocks, a.max_blocks_per_req, a.dst_max_blocks, a.first, a.recent = 2, 2, 128, 16, 4, 2, 4, 8
     a.kv_dtype, a.kv_layout = sv.SPEC_INT8, sv.KV_MFMA
-    _fake(a, "k_cache", "v_cache", "kv_scale", "weight", "block_table", "kv_len", "keep", "new_kv_len", "kept")
-    a.dst_block_table = FAKE * 2
+    _fake(a, "k_cache", "v_cache", "kv_scale", "weight", "block_table", "kv_len", "keep", "kept")
+    a.dst_block_table, a.new_kv_len = FAKE * 2, FAKE << 8
     a.host_kv_len = hk.ctypes.data
     a._keep = (hk,)
     return a
@@ -96,6 +96,7 @@ E, U = sv.SPEC_EINVAL, sv.SPEC_EUNSUPPORTED
     (_set(out_k=None), E), (_set(positions=None), E), (_set(inv_freq=None), E), (_set(q=FAKE + 8), E), (_set(out_q=FAKE + 4), E), (_set(k_weight=FAKE + 2), E),
     (_set(q_stride=1023), E), (_set(q_stride=1028), E), (_set(out_k_stride=128), E), (_set(d=96, rot_dim=96), U), (_set(rot_dim=24), U),
     (_set(T=1 << 30), U), (_set(T=(1 << 25) + 1, Hq=1, Hkv=1), U),
+    (_set(out_q_stride=1032), E), (_set(q_stride=2048), E), (_set(k_stride=1024), E), (_set(k_stride=1024, out_k_stride=1032), E),   # (in place, but other tokens apart)
 ])
 def test_rope_refuses(mutate, status):
     a = _rope()
@@ -126,6 +127,7 @@ def test_prompt_attn_refuses(mutate, status):
 
 @pytest.mark.parametrize("mutate,status", ROWS + [
     (_set(weight=None), E), (_set(lse=None), E), (_set(weight=FAKE + 8), E), (_set(weight_in=FAKE + 8), E), (_set(lse=FAKE + 1), E),
+    (_set(weight_in=FAKE + 16 * 2 * 64 - 32), E), (_set(weight_in=FAKE - 32), E),
 ])
 def test_kv_weight_refuses(mutate, status):
     a = _weight()
@@ -134,6 +136,7 @@ def test_kv_weight_refuses(mutate, status):
 
 
 @pytest.mark.parametrize("mutate,status", [
+    (_set(new_kv_len=FAKE), E), (_set(new_kv_len=FAKE + 4), E), (_set(kv_len=(FAKE << 8) + 4), E), (_set(keep=FAKE << 8), E),   # (lengths out over lengths in)
     (_set(B=0), E), (_set(Hkv=0), E), (_set(num_blocks=0), E), (_set(dst_max_blocks=0), E), (_set(first=-1), E), (_set(recent=-1), E), (_set(k_cache=None), E),
     (_set(weight=None), E), (_set(keep=None), E), (_set(new_kv_len=None), E), (_set(dst_block_table=None), E), (_set(dst_block_table=FAKE), E),
     (_set(kv_scale=None), E), (_set(kv_dtype=sv.SPEC_BF16), E), (_set(kv_dtype=sv.SPEC_F32, kv_scale=None), E), (_set(kv_dtype=7), E),
@@ -271,3 +274,12 @@ def test_evict_binding_refuses():
                dict(new=_i32(0)), dict(kept=torch.zeros((2, 17), dtype=torch.int32)), dict(kept=torch.zeros((1, 16), dtype=torch.int32)), dict(k=k[:, :, :8])):
         with pytest.raises((ValueError, TypeError)):
             make(**kw)
+
+
+@pytest.mark.parametrize("wrong", [dict(requests=0), dict(prompt=(0, 9)), dict(prompt=(9, 8)), dict(chunk=0), dict(budget=0), dict(window=0), dict(first=-1), dict(k=-1)])
+def test_prompt_loop_refuses(wrong):
+    from paper_2406_14066_amd.prompt_loop import PromptLoop
+    given = dict(requests=1, prompt=(8, 9), budget=4, chunk=8)
+    given.update(wrong)
+    with pytest.raises(ValueError):
+        PromptLoop(given.pop("requests"), given.pop("prompt"), device="cpu", **given)
