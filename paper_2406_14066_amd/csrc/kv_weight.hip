@@ -7,23 +7,27 @@ namespace specv {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr int kWeightWaves = 4, kTileRows = 32;
+constexpr int kTileRows = 32;
+constexpr int waves_of(int form) { return form == kWeightSome ? 8 : 4; }
 
 // 32 tokens of a request and KV head are a wavefront's, or, where there are too few of them for the device (kWeightShared), a block's, whose
 // wavefronts take the rows in turn.  The query rows that see any of the block's tokens pass through LDS, 64 (shared: 128) at a time, as rows: read from
-// memory in operand order they would be 64 lanes in 64 cache lines each time (32 rows of four requests of 4500 .. 9400 tokens, 64/8 heads: 42 us, with rows in LDS 28).
+// memory in operand order they would be 64 lanes in 64 cache lines each time (32 rows of four requests of 4500 .. 9400 tokens, 64/8 heads: 42 us, with rows in LDS 28, all of them at once 22).
 // S[row][token] = Q[row][:] . K[token][:] with v_mfma_f32_32x32x16_bf16, K's 32 tokens held in registers: lane (half, c) holds token c,
 // rows 8 i + 4 half .. + 3, so that a token's sum is the lane's own additions, one exchange with the other half, and
 // (shared) four wavefronts through LDS, in a fixed order.
 // kWeightFew: at most 64 rows, a step's: they stay in LDS, and the wavefronts go through several groups of tokens whose K is asked for two groups
 // ahead; nothing in between waits for a load (five rows of 64 requests, 1000 .. 3000 tokens of e4m3: 40 us for 150 MB, 3.8 TB/s; one group a block 55).
+// kWeightSome: at most 256 rows, the same with eight wavefronts a block and K asked for where the group before it ends, which leaves registers for four wavefronts
+// a SIMD (a group ahead: 24 us instead of 22).  Bound by the exponentials and their sums (32 rows of four requests of 4500 .. 9400 tokens: about 13 us of the 22).
 template <int KIND, int D, int FORM>
-__global__ __launch_bounds__(kWeightWaves *kWave, 2) void kv_weight_kernel(KvWeightParams p)
+__global__ __launch_bounds__(waves_of(FORM) *kWave, FORM == kWeightSome ? 4 : 2) void kv_weight_kernel(KvWeightParams p)
 {
-    constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, SHARED = FORM == kWeightShared, FEW = FORM == kWeightFew;
-    constexpr int kAhead = FEW ? 2 : 1;     // groups whose K is asked for ahead
+    constexpr bool B8 = is_8bit(KIND), INT8 = KIND == kCacheInt8, SHARED = FORM == kWeightShared, SOME = FORM == kWeightSome, FEW = FORM == kWeightFew || SOME;
+    constexpr int kWeightWaves = waves_of(FORM);
+    constexpr int kAhead = FORM == kWeightFew ? 2 : 1;     // groups whose K is asked for ahead
     constexpr int KS = D / 16, kPageBytes = SPEC_BLOCK_SIZE * D * (B8 ? 1 : 2);
-    constexpr int kThreads = kWeightWaves * kWave, kRows = SHARED ? 128 : 64, kStageTiles = kRows / kTileRows, kRowBytes = D * 2 + 16;
+    constexpr int kThreads = kWeightWaves * kWave, kRows = SOME ? kWeightSomeRows : SHARED ? 128 : kWeightFewRows, kStageTiles = kRows / kTileRows, kRowBytes = D * 2 + 16;
     constexpr int kRowPieces = D / 8, kPieces = kRows * kRowPieces / kThreads;   // 16-byte pieces of a row, of a thread
     constexpr int kBuffers = FEW ? 1 : 2;
     __shared__ alignas(16) unsigned char rows[kBuffers][kRows * kRowBytes];
@@ -36,7 +40,7 @@ __global__ __launch_bounds__(kWeightWaves *kWave, 2) void kv_weight_kernel(KvWei
     const int place = (int)(blockIdx.x / (unsigned)p.Hkv), kvh = (int)blockIdx.x - place * p.Hkv, b = blockIdx.y;
     const int row0 = uniform_load(p.cu_q_len, b), end = uniform_load(p.cu_q_len, b + 1), kv_len = uniform_load(p.kv_len, b);
     if (row0 < 0 || end <= row0 || end > p.T) return;
-    // (kWeightFew is chosen by the host's offsets: rows beyond a stage's, from others in device memory, would be lost)
+    // (kWeightFew and kWeightSome are chosen by the host's offsets: rows beyond a stage's, from others in device memory, would be lost)
     if (kv_len < 0 || kv_len > p.capacity_tokens || (kv_len + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE > p.max_blocks_per_req ||
         (FEW && (end - row0) * p.group > kRows)) {
         if (blockIdx.x == 0 && tid == 0 && p.errors != nullptr) atomicAdd(p.errors, 1ull);
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(kWeightWaves *kWave, 2) void kv_weight_kernel(KvWei
             }
         }
         const float old = before[at_ring];
-        if (FEW) load_k(group + kAhead, at_ring);
+        if (FEW && !SOME) load_k(group + kAhead, at_ring);
         float sum = 0.0f;
         for (int stage = first_stage, buf = 0; stage < (FEW ? 1 : stages); ++stage, buf ^= FEW ? 0 : 1) {
             if (!FEW) {
@@ -180,6 +184,7 @@ __global__ __launch_bounds__(kWeightWaves *kWave, 2) void kv_weight_kernel(KvWei
                 }
             }
         }
+        if (SOME) load_k(group + kAhead, at_ring);
         const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
         sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
         if constexpr (SHARED) {   // (one group)
@@ -204,9 +209,10 @@ __global__ __launch_bounds__(kWeightWaves *kWave, 2) void kv_weight_kernel(KvWei
 template <int KIND, int D>
 void go(const KvWeightParams &p, hipStream_t stream)
 {
-    const unsigned each = p.form == kWeightShared ? 1u : kWeightWaves * (p.form == kWeightFew ? (unsigned)p.groups : 1u);   // times 32 tokens of a block
-    const dim3 grid(((unsigned)p.max_tiles + each - 1) / each * (unsigned)p.Hkv, (unsigned)p.B), threads(kWeightWaves * kWave);
+    const unsigned waves = (unsigned)waves_of(p.form), each = p.form == kWeightShared ? 1u : waves * (p.form >= kWeightFew ? (unsigned)p.groups : 1u);   // times 32 tokens of a block
+    const dim3 grid(((unsigned)p.max_tiles + each - 1) / each * (unsigned)p.Hkv, (unsigned)p.B), threads(waves * kWave);
     if (p.form == kWeightShared) hipLaunchKernelGGL((kv_weight_kernel<KIND, D, kWeightShared>), grid, threads, 0, stream, p);
+    else if (p.form == kWeightSome) hipLaunchKernelGGL((kv_weight_kernel<KIND, D, kWeightSome>), grid, threads, 0, stream, p);
     else if (p.form == kWeightFew) hipLaunchKernelGGL((kv_weight_kernel<KIND, D, kWeightFew>), grid, threads, 0, stream, p);
     else hipLaunchKernelGGL((kv_weight_kernel<KIND, D, kWeightOwn>), grid, threads, 0, stream, p);
 }

@@ -199,7 +199,7 @@ spec_status check_weight(const spec_kv_weight_args *a)
     return st;
 }
 
-constexpr int kWeightFewWaves = 16;   // wavefronts a compute unit that blocks of several groups of tokens leave at least
+constexpr int kWeightFewWaves = 16;   // wavefronts a compute unit that kWeightFew's blocks of several groups of tokens leave at least
 
 spec_status check_evict(const spec_kv_evict_args *a)
 {
@@ -323,8 +323,22 @@ spec_status spec_kv_weight(const spec_kv_weight_args *a, void *hip_stream)
         most_rows = std::max(most_rows, n * p.group);
         if (n > 0) units += (int64_t)((a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) + kWeightTokens - 1) / kWeightTokens * a->Hkv;
     }
-    p.form = most_rows <= kWeightFewRows ? kWeightFew : units < 8 * compute_units() ? kWeightShared : kWeightOwn;
+    // A block for each 32 tokens as long as all of them run at once (two a unit): 32 rows of 64/8 heads behind 500 tokens 5.9 us against 9.2 and 9.3 of the
+    // other two forms, 2000 tokens 6.4, 9.7, 9.3; 4000 tokens 11.2, 9.7, 9.6.  Rows that fit LDS stay there: four requests of 4000 .. 12000 tokens 22 against 27.
+    p.form = most_rows <= kWeightFewRows ? kWeightFew : units <= 2 * compute_units() ? kWeightShared : most_rows <= kWeightSomeRows ? kWeightSome : kWeightOwn;
     p.groups = (int)std::min<int64_t>(std::max<int64_t>(units / (kWeightFewWaves * compute_units()), 1), 16);
+    if (p.form == kWeightSome) {
+        // As few groups as let all blocks run at once (two a unit), else two: four requests of 4500 .. 9400 tokens, by groups: 25.3, 22.1 *, 27.2, 33.8; of 8500: 30.8, 32.2, 28.7 *,
+        // 34.1; two of 30000, int8: 44.2, 40.9, -, 39.8 *; 32/8 heads, sixteen of 4000 .. 12000: 73, 63.7 *, -, 64.6.
+        auto blocks = [&](int groups) {
+            int64_t n = 0;
+            for (int b = 0; b < a->B; ++b)
+                if (a->host_cu_q_len[b + 1] > a->host_cu_q_len[b]) n += (a->max_kv_len > 0 ? a->max_kv_len : a->host_kv_len[b]) / (8 * kWeightTokens * groups) + 1;
+            return n * a->Hkv;
+        };
+        for (p.groups = 1; p.groups < 5 && blocks(p.groups) > 2 * compute_units(); ++p.groups) {}
+        if (p.groups == 5) p.groups = 2;
+    }
     p.group_inverse = inverse_of_group(p.group);
     p.scale_log2 = scale_log2_of(a->softmax_scale, a->d);
     p.q_stride = a->q_token_stride != 0 ? a->q_token_stride : (int64_t)a->Hq * a->d;

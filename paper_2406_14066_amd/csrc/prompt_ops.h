@@ -50,13 +50,14 @@ enum : int32_t {
     kWeightOwn = 0,      // a block's wavefronts have tokens of their own and go through the same rows
     kWeightShared = 1,   // ... have the same tokens and share the rows
     kWeightFew = 2,      // at most kWeightFewRows rows: they stay in LDS, and the wavefronts go through many tokens
+    kWeightSome = 3,     // ... kWeightSomeRows
 };
-constexpr int kWeightFewRows = 64;
+constexpr int kWeightFewRows = 64, kWeightSomeRows = 256;
 struct KvWeightParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, kind;
     int32_t d, max_tiles, capacity_tokens;
     int32_t form;           // one of kWeight*
-    int32_t groups;         // kWeightFew: times 128 tokens that a block takes one after another
+    int32_t groups;         // kWeightFew, kWeightSome: times 32 tokens that a wavefront takes one after another
     uint32_t group_inverse;
     float scale_log2;
     int32_t reserved;

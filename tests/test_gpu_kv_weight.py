@@ -72,6 +72,11 @@ CASES = [
     ("empty_rows", [3, 70, 0, 1, 2], [0, 2, 50, 0, 2], 8, 4, 128, 0.0),
     ("group_16", [20], [333], 16, 1, 64, 0.0),
     ("sharp", [40], [140], 4, 4, 128, 3.0),
+    # tokens enough for wavefronts with tokens of their own: rows that all stay in LDS, for several groups of tokens, and more rows
+    ("some_rows", [100, 37, 0, 128, 1], [1100, 1025, 40, 128, 33], 32, 16, 128, 0.0),
+    ("some_rows_groups", [20, 40], [9000, 7533], 32, 16, 64, 0.0),
+    ("many_rows", [300, 20, 129], [1100, 1025, 700], 32, 16, 64, 0.0),
+    ("many_rows_d128", [520], [1101], 20, 20, 128, 0.0),
 ]
 
 
