@@ -116,7 +116,7 @@ spec_status check_prompt(const spec_prompt_attn_args *a)
 // heads: 8 86, 16 52, 32 38 *, 64 45; 8 requests of 1 .. 9 rows behind 2000 .. 30000: 4 131, 8 104 *, 12 101, 24 109; 512 rows behind 8000: 1 206, 2 140 *, 3 167;
 // a prompt of 4000 tokens: 1 130 *, 2 156, 4 189.
 struct PromptPlan {
-    int rows_log2, items, chunk_tokens, max_chunks, capacity;
+    int rows_log2, items, chunk_tokens, max_chunks, even, capacity;
     size_t acc, ml, total;   // offsets into the workspace
 };
 constexpr int kStep = 64;
@@ -147,6 +147,7 @@ PromptPlan plan_prompt(const spec_prompt_attn_args *a, bool whole)
     int best = most_steps;
     double best_cost = 1e300;
     pl.rows_log2 = 7;
+    pl.even = 1;
     for (int wide = 0; wide <= (a->d == 128 && padded[1] <= 1.1 * padded[0] ? 1 : 0); ++wide) {
         const double slots = units * (wide ? 1.0 : 2.0), together = wide ? 1.0 : kTogether;
         for (int chunks = 1, last = 0; chunks <= (whole ? 1 : kMostPromptChunks); chunks = std::max(chunks + 1, chunks * 5 / 4)) {
@@ -169,6 +170,34 @@ PromptPlan plan_prompt(const spec_prompt_attn_args *a, bool whole)
                 best = length;
                 pl.rows_log2 = 7 + wide;
             }
+        }
+    }
+    // Wide blocks, more than half as many as there are units: the longest are cut, and units left over take what remains of them, two of those
+    // each and with time to spare (blocks are handed to parts of the device in turn, whichever is free).  Four chunks of 340 .. 421 rows behind 7100 .. 9800 tokens
+    // of e4m3, 208 blocks of 118 .. 159 steps, by the steps of a first piece: 159 308, 145 293, 135 277, 124 260 *, 119 (every request cut) 303; halves 326.
+    // (Blocks of 128 rows, two a unit: between 0.94 and 1.09 of the time, and are left alone.)
+    double first = 0.0;
+    const double best_even = best_cost;
+    each_request([&](int64_t rows, int, int) { first += (double)((rows + 255) >> 8) * a->Hkv; });
+    const bool cut = a->d == 128 && padded[1] <= 1.1 * padded[0] && !whole && first > 0.5 * units && first < units;
+    for (int part = 1; part <= 16 && cut; ++part) {
+        const int length = most_steps - most_steps * part / 32;
+        double rests = 0.0, rest = 0.0, bytes = 0.0;
+        each_request([&](int64_t rows, int tokens, int) {
+            const int steps = (tokens + kStep - 1) / kStep;
+            if (steps <= length) return;
+            const double blocks = (double)((rows + 255) >> 8) * a->Hkv;
+            rests += blocks;
+            rest += blocks * (steps - length + kBlockSteps);
+            bytes += (double)rows * a->Hkv * 2 * a->d * 8.0;
+        });
+        if (rests == 0.0 || rests > 2.0 * (units - first) || rest > 0.6 * (units - first) * length) continue;
+        const double cost = kWideStepUs * (length + kBlockSteps) + kJoinUs + 2 * kJoinChunkUs + bytes / kJoinBytesPerUs;
+        if (cost < best_cost && cost < 0.93 * best_even) {
+            best_cost = cost;
+            best = length;
+            pl.rows_log2 = 8;
+            pl.even = 0;
         }
     }
     pl.items = row_item(a->T, a->B, group, pl.rows_log2);
@@ -291,7 +320,7 @@ spec_status spec_prompt_attn(const spec_prompt_attn_args *a, void *workspace, si
     p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.group = a->Hq / a->Hkv; p.num_blocks = a->num_blocks; p.max_blocks_per_req = a->max_blocks_per_req; p.T = a->T;
     p.kind = kind_of(a->kv_dtype, a->kv_layout);
     p.d = a->d; p.out_f32 = a->out_dtype == SPEC_F32;
-    p.rows_log2 = pl.rows_log2; p.items = pl.items; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks; p.capacity_tokens = pl.capacity;
+    p.rows_log2 = pl.rows_log2; p.items = pl.items; p.even = pl.even; p.chunk_tokens = pl.chunk_tokens; p.max_chunks = pl.max_chunks; p.capacity_tokens = pl.capacity;
     p.group_inverse = inverse_of_group(p.group);
     p.scale_log2 = scale_log2_of(a->softmax_scale, a->d);
     p.q_stride = a->q_token_stride != 0 ? a->q_token_stride : (int64_t)a->Hq * a->d;

@@ -140,7 +140,9 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     const int chunks = chunks_of(seen, p.chunk_tokens), chunk = blockIdx.y;
     if (chunk >= chunks) return;
     const int all_steps = (seen + kStepTokens - 1) / kStepTokens;
-    const int first_step = (int)((int64_t)all_steps * chunk / chunks), steps = (int)((int64_t)all_steps * (chunk + 1) / chunks) - first_step;
+    // (even shares, or whole chunks and what is left)
+    const int first_step = p.even ? (int)((int64_t)all_steps * chunk / chunks) : chunk * (p.chunk_tokens / kStepTokens);
+    const int steps = (p.even ? (int)((int64_t)all_steps * (chunk + 1) / chunks) : min(first_step + p.chunk_tokens / kStepTokens, all_steps)) - first_step;
     const int tok0 = first_step * kStepTokens, tok1 = min(seen, tok0 + steps * kStepTokens);
 
     // this wavefront's rows: lane c32 holds row row_lo + c32, which sees the tokens up to `limit`

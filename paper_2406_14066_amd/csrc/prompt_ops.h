@@ -29,7 +29,7 @@ constexpr int kMostPromptChunks = 64;   // of a row's tokens
 // items row_item(cu[b], b) .. row_item(cu[b + 1], b + 1) - 1 of the grid, which are enough for its row blocks; those left over have no work.
 struct PromptAttnParams {
     int32_t B, Hq, Hkv, group, num_blocks, max_blocks_per_req, T, kind;
-    int32_t d, out_f32, rows_log2, items, chunk_tokens, max_chunks, capacity_tokens;
+    int32_t d, out_f32, rows_log2, items, chunk_tokens, max_chunks, even, capacity_tokens;
     uint32_t group_inverse;
     float scale_log2;
     int32_t reserved;

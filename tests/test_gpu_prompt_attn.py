@@ -393,6 +393,20 @@ def test_a_batch_that_fills_the_device():
     assert errors == 0
 
 
+@pytest.mark.parametrize("kind,out", [("tiles", "f32"), ("e4m3", "bf16")])
+def test_one_request_much_longer_than_the_others(kind, out):
+    """On a device of 256 units its rows' tokens are cut in a whole chunk and a rest, which units without a block take."""
+    rng = np.random.default_rng(24)
+    q_len, kv_len, Hq, Hkv, d = [256, 250, 256, 256, 251, 255, 256], [1597, 1000, 1100, 1080, 900, 1100, 1050], 32, 8, 128
+    table, nb = R.tables(rng, kv_len)
+    cache = R.Cache(rng, nb, Hkv, d, kind)
+    cu = R.prefix_sum(q_len)
+    q = rng.standard_normal((int(cu[-1]), Hq, d))
+    got, lse, errors = run(cache, q, table, kv_len, cu, out)
+    check(got, lse, reference(cache, q, table, kv_len, cu), out, kind, d)
+    assert errors == 0
+
+
 @pytest.mark.parametrize("scale", [1e3, 1e7])
 def test_very_negative_scores(scale):
     """The softmax is that of the differences."""
