@@ -33,6 +33,8 @@ CACHE_PARTS = 5
 # prompt_attn.hip: likewise (SPEC_PROMPT_PART)
 PROMPT_KERNEL = "prompt_attn.hip"
 PROMPT_PARTS = 5
+# sources that tell fp32's denormals apart (those of accumulated weights)
+DENORMAL_SOURCES = ("kv_evict.hip",)
 
 
 def compile_jobs(objdir: str):
@@ -43,16 +45,17 @@ def compile_jobs(objdir: str):
     jobs = []
     for src in sources():
         stem = os.path.splitext(os.path.basename(src))[0]
+        compiler = base + (["-fno-gpu-flush-denormals-to-zero"] if os.path.basename(src) in DENORMAL_SOURCES else [])
         name, parts = {STEP_KERNEL: ("SPEC_STEP_PART", STEP_PARTS),
                        CACHE_KERNEL: ("SPEC_CACHE_PART", CACHE_PARTS),
                        PROMPT_KERNEL: ("SPEC_PROMPT_PART", PROMPT_PARTS)}.get(os.path.basename(src), (None, 0))
         if parts:
             for part in range(parts):
                 obj = os.path.join(objdir, "%s_part%d.o" % (stem, part))
-                jobs.append((base + ["-D%s=%d" % (name, part), "-o", obj, src], obj))
+                jobs.append((compiler + ["-D%s=%d" % (name, part), "-o", obj, src], obj))
         else:
             obj = os.path.join(objdir, stem + ".o")
-            jobs.append((base + ["-o", obj, src], obj))
+            jobs.append((compiler + ["-o", obj, src], obj))
     return jobs
 
 

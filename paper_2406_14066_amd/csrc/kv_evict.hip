@@ -11,21 +11,11 @@ constexpr int kScoreWaves = 4, kChoiceThreads = kEvictTurn / 4, kChoiceWaves = k
 
 constexpr uint32_t kNoScore = 1, kProtected = 0xFFFFFFFFu;   // below and above every score; 0: no token there
 
-// (The library flushes fp32's denormals, and weights may be: their conversions to 64 bits and back are done on the bits.)
-__device__ __forceinline__ double wide(float x)
-{
-    const uint32_t bits = __float_as_uint(x);
-    if ((bits & 0x7F800000u) != 0) return (double)x;
-    const double v = (double)(bits & 0x7FFFFFu) * 0x1p-149;
-    return bits >> 31 ? -v : v;
-}
 // A score as a word that orders like it, kNoScore for NaN: the sum rounded to fp32, both zeros alike.
 __device__ __forceinline__ uint32_t ordered(double x)
 {
     if (!(x == x)) return kNoScore;
-    uint32_t bits;
-    if (fabs(x) < 0x1p-126) bits = (uint32_t)rint(fabs(x) * 0x1p149) | (x < 0.0 ? 0x80000000u : 0u);
-    else bits = __float_as_uint((float)x);
+    uint32_t bits = __float_as_uint((float)x);   // (this file is compiled with fp32's denormals: small weights are told apart)
     if (bits == 0x80000000u) bits = 0;
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
@@ -52,7 +42,7 @@ __device__ __forceinline__ uint32_t score_of(const KvEvictParams &p, int entry, 
     const float *from = p.weight + (size_t)entry * p.Hkv * SPEC_BLOCK_SIZE + slot;
     double sum = 0.0;
 #pragma unroll 8
-    for (int h = 0; h < p.Hkv; ++h) sum += wide(from[h * SPEC_BLOCK_SIZE]);
+    for (int h = 0; h < p.Hkv; ++h) sum += (double)from[h * SPEC_BLOCK_SIZE];
     return ordered(sum);
 }
 
@@ -73,7 +63,7 @@ __global__ __launch_bounds__(kScoreWaves *kWave) void evict_score_kernel(KvEvict
 }
 
 // A block per request: the smallest score that stays is found from counts over 2048 even parts of the interval that it lies in, first that of all
-// scores, then the part in which it was found, and so on (three times at the most); then the tokens that stay find their places from the numbers,
+// scores, then the part in which it was found, and so on (three times at the most, fewer where all of a part stays); then the tokens that stay find their places from the numbers,
 // before them, of scores above it and at it (of which the earliest stay).  A thread has 4 * HELD tokens side by side; they are in
 // registers throughout, or, longer requests (LONG), fetched again for each pass.  HELD == 1 makes the scores itself.
 // What is handed to the copies is where a token lies: page * 16 + slot, -1 outside the pool.
@@ -124,7 +114,7 @@ __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictPar
                 for (int h = 0; h < p.Hkv; ++h) {
                     const f32x4 w = *reinterpret_cast<const f32x4 *>(from + h * SPEC_BLOCK_SIZE);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] += wide(w[e]);
+                    for (int e = 0; e < 4; ++e) sum[e] += (double)w[e];
                 }
             }
 #pragma unroll
@@ -207,7 +197,7 @@ __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictPar
             for (int e = 0; e < 2; ++e) {
                 if (over < rest && over + mine[e] >= rest) {
                     found_digit = kBins - 1 - 2 * tid - e;
-                    found_rest = rest - over;
+                    found_rest = over + mine[e] == rest ? 0 : rest - over;
                 }
                 over += mine[e];
             }
@@ -216,6 +206,10 @@ __global__ __launch_bounds__(kChoiceThreads) void evict_choice_kernel(KvEvictPar
             least += from;
             span = min(span - from, (1u << shift) - 1u);
             rest = found_rest;
+            if (rest == 0) {   // all of the part stays: whatever is above the score before its first
+                least -= 1;
+                break;
+            }
             if (shift == 0) break;
             __syncthreads();   // (found_* and the counts have been read)
         }
