@@ -25,7 +25,7 @@ def test_prompt_kernels_use_no_private_memory_and_two_wavefronts_fit_a_simd(tmp_
         return subprocess.run(cmd, check=True, capture_output=True, text=True).stderr
 
     jobs = [(B.PROMPT_KERNEL, ["-DSPEC_PROMPT_PART=%d" % part]) for part in range(B.PROMPT_PARTS)] + [
-        (name, []) for name in ("kv_weight.hip", "kv_evict.hip", "qk_norm_rope.hip")]
+        (name, ["-fno-gpu-flush-denormals-to-zero"] if name in B.DENORMAL_SOURCES else []) for name in ("kv_weight.hip", "kv_evict.hip", "qk_norm_rope.hip")]
     with ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 4)) as pool:
         logs = list(pool.map(compile_one, jobs))
     kernels, name = {}, None
