@@ -15,7 +15,8 @@ constexpr int waves_of(int form) { return form == kWeightSome ? 8 : 4; }
 // memory in operand order they would be 64 lanes in 64 cache lines each time (32 rows of four requests of 4500 .. 9400 tokens, 64/8 heads: 42 us, with rows in LDS 28, all of them at once 22).
 // S[row][token] = Q[row][:] . K[token][:] with v_mfma_f32_32x32x16_bf16, K's 32 tokens held in registers: lane (half, c) holds token c,
 // rows 8 i + 4 half .. + 3, so that a token's sum is the lane's own additions, one exchange with the other half, and
-// (shared) four wavefronts through LDS, in a fixed order.
+// (shared) four wavefronts through LDS, in a fixed order.  A tile's 16 weights of a lane are added in a few levels, and tiles, of which a long prompt has thousands, with
+// what each addition loses kept (one after another, 48000 weights of about the same size lost 1e-4 of their sum, all in one direction).
 // kWeightFew: at most 64 rows, a step's: they stay in LDS, and the wavefronts go through several groups of tokens whose K is asked for two groups
 // ahead; nothing in between waits for a load (five rows of 64 requests, 1000 .. 3000 tokens of e4m3: 40 us for 150 MB, 3.8 TB/s; one group a block 55).
 // kWeightSome: at most 256 rows, the same with eight wavefronts a block and K asked for where the group before it ends, which leaves registers for four wavefronts
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(waves_of(FORM) *kWave, FORM == kWeightSome ? 4 : 2)
         }
         const float old = before[at_ring];
         if (FEW && !SOME) load_k(group + kAhead, at_ring);
-        float sum = 0.0f;
+        float sum = 0.0f, lost = 0.0f;   // so far; what its additions have lost
         for (int stage = first_stage, buf = 0; stage < (FEW ? 1 : stages); ++stage, buf ^= FEW ? 0 : 1) {
             if (!FEW) {
                 store_rows(buf);
@@ -167,24 +168,34 @@ __global__ __launch_bounds__(waves_of(FORM) *kWave, FORM == kWeightSome ? 4 : 2)
                 for (int ks = 0; ks < KS; ++ks)
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                         *reinterpret_cast<const bf16x8 *>(row + (B8 ? 64 * (ks / 2) + 32 * half + 16 * (ks % 2) : 32 * ks + 16 * half)), k[ks], s, 0, 0, 0);
+                f32x4 parts = {0.0f, 0.0f, 0.0f, 0.0f};   // of the tile's 16 weights
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
                     const int at4 = i * kTileRows + 8 * e4 + 4 * half;
                     const f32x4 off = *reinterpret_cast<const f32x4 *>(&row_lse[buf][at4]);
                     if (all_see) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sum += fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
+                        for (int e = 0; e < 4; ++e) parts[e] += fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float x = fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
-                            sum += row_limit[buf][at4 + e] >= t0 + c32 ? x : 0.0f;
+                            parts[e] += row_limit[buf][at4 + e] >= t0 + c32 ? x : 0.0f;
                         }
                     }
+                }
+                const float tile = (parts[0] + parts[1]) + (parts[2] + parts[3]);
+                if constexpr (FEW) {
+                    sum += tile;
+                } else {
+                    const float add = tile - lost, next = sum + add;
+                    lost = next < INFINITY ? (next - sum) - add : 0.0f;   // (rows with an lse of other scores: infinite weights stay infinite)
+                    sum = next;
                 }
             }
         }
         if (SOME) load_k(group + kAhead, at_ring);
+        if (!FEW) sum -= lost;
         const u32x2_t both = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
         sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
         if constexpr (SHARED) {   // (one group)
