@@ -287,7 +287,9 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     };
 
     f32x16 acc[SL];
-    float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;   // the reference, what it is while no key has been seen, the lane's part of the sum
+    float m_run = -INFINITY, m_use = 0.0f;     // the reference, and what it is while no key has been seen
+    float l_run = 0.0f, l_lost = 0.0f;         // the lane's part of the sum, what its additions have lost
+    f32x4 l_step = {0.0f, 0.0f, 0.0f, 0.0f};   // parts of the step's
 #pragma unroll
     for (int sl = 0; sl < SL; ++sl)
 #pragma unroll
@@ -357,6 +359,7 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
             const bool up = mx > m_run + kRescaleSlack;
             const float alpha = up ? fast_exp2(m_run - mx) : 1.0f;
             l_run *= alpha;
+            l_lost *= alpha;
 #pragma unroll
             for (int sl = 0; sl < SL; ++sl) acc[sl] *= alpha;
             if (up) m_run = m_use = mx;
@@ -372,8 +375,9 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
             for (int r = 0; r < 4; ++r) {
                 const float x = s[h][4 * i + r];
                 const float e = fast_exp2(B8 ? x - m_use : fmaf(x, p.scale_log2, -m_use));
-                if constexpr (B8) l_run = fmaf(e, rv[r], l_run);
-                else l_run += e;
+                const float part = h + i > 0 ? l_step[r] : 0.0f;
+                if constexpr (B8) l_step[r] = fmaf(e, rv[r], part);
+                else l_step[r] = part + e;
                 float rest = e;
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) {
@@ -381,6 +385,11 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
                     if (t + 1 < TERMS) rest -= (float)pw[h][i / 2][t][4 * (i % 2) + r];
                 }
             }
+        }
+        if (h == 1) {   // a step's weights in a few levels, and steps with what each addition loses: thousands of equal ones would lose the same each time
+            const float add = ((l_step[0] + l_step[1]) + (l_step[2] + l_step[3])) - l_lost, next = l_run + add;
+            l_lost = (next - l_run) - add;
+            l_run = next;
         }
     };
     // product of pair h's weights with its V in buffer `buf`
@@ -455,6 +464,7 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     for (; u < steps; ++u) walk(u, std::true_type{});
 
     // Results, and partial results where the tokens are split, go through LDS so that they go out in long pieces.
+    l_run -= l_lost;
     l_run += __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false)[half ^ 1]);
     const bool whole = chunks == 1;
     const size_t my_index = packed_row(p, row0, kvh, my_row);
