@@ -526,8 +526,9 @@ typedef struct {
     float *lse;                   /* optional [T][Hq]: natural logarithm of the sum of exp(scaled scores) */
     const int32_t *host_kv_len;   /* HOST copies (host_kv_len may be NULL if max_kv_len > 0) */
     const int32_t *host_cu_q_len;
-    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths do not
-                                     fit the launch (their rows are not written), and block-table entries outside
+    int64_t *error_count;         /* optional DEVICE counter [1], ADDED to: requests left out because their lengths, or their row offsets in device
+                                     memory, do not fit the launch (their rows are not written; offsets that do not ascend may keep rows of
+                                     the requests about them from being written too), and block-table entries outside
                                      [0, num_blocks) (such a page reads as zeros) */
     float softmax_scale;          /* 0 means 1/sqrt(d) */
 } spec_prompt_attn_args;

@@ -40,9 +40,9 @@ __global__ __launch_bounds__(waves_of(FORM) *kWave, FORM == kWeightSome ? 4 : 2)
     const int half = lane >> 5, c32 = lane & 31;
     const int place = (int)(blockIdx.x / (unsigned)p.Hkv), kvh = (int)blockIdx.x - place * p.Hkv, b = blockIdx.y;
     const int row0 = uniform_load(p.cu_q_len, b), end = uniform_load(p.cu_q_len, b + 1), kv_len = uniform_load(p.kv_len, b);
-    if (row0 < 0 || end <= row0 || end > p.T) return;
+    if (end == row0) return;
     // (kWeightFew and kWeightSome are chosen by the host's offsets: rows beyond a stage's, from others in device memory, would be lost)
-    if (kv_len < 0 || kv_len > p.capacity_tokens || (kv_len + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE > p.max_blocks_per_req ||
+    if (!offsets_fit(row0, end, p.T) || kv_len < 0 || kv_len > p.capacity_tokens || (kv_len + SPEC_BLOCK_SIZE - 1) / SPEC_BLOCK_SIZE > p.max_blocks_per_req ||
         (FEW && (end - row0) * p.group > kRows)) {
         if (blockIdx.x == 0 && tid == 0 && p.errors != nullptr) atomicAdd(p.errors, 1ull);
         return;

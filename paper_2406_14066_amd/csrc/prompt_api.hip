@@ -313,7 +313,7 @@ spec_status spec_prompt_attn(const spec_prompt_attn_args *a, void *workspace, si
     if (workspace_bytes < pl.total) pl = plan_prompt(a, true);   // (sized for another call: tokens are not split)
     if (workspace_bytes < pl.total) return SPEC_EWORKSPACE;
     if (a->T == 0) return SPEC_OK;
-    if ((int64_t)pl.items * a->Hkv * (2 << pl.rows_log2) >= kMostThreads) return SPEC_EUNSUPPORTED;   // (two threads a row)
+    if (((int64_t)pl.items * a->Hkv + 1) * (2 << pl.rows_log2) >= kMostThreads) return SPEC_EUNSUPPORTED;   // (two threads a row)
     char *ws = static_cast<char *>(workspace);
     PromptAttnParams p;
     memset(&p, 0, sizeof p);

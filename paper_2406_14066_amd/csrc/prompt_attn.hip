@@ -123,6 +123,16 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     const int half = lane >> 5, c32 = lane & 31, n16 = lane & 15, g = lane >> 4;
     const int item = (int)(blockIdx.x / (unsigned)p.Hkv), kvh = (int)blockIdx.x - item * p.Hkv;
 
+    // Offsets that lie outside the rows may be no request's that an item leads to: one block, behind all items, looks at them.
+    if (item >= p.items) {
+        if (blockIdx.y == 0)
+            for (int b = tid; b < p.B; b += W * kWave) {
+                const unsigned long long found = __builtin_amdgcn_ballot_w64(!offsets_fit(p.cu_q_len[b], p.cu_q_len[b + 1], p.T));
+                if (found != 0 && lane == __builtin_ctzll(found)) atomicAdd(p.errors, (unsigned long long)__builtin_popcountll(found));
+            }
+        return;
+    }
+
     // the row block and its tokens
     const int b = request_of_rows(p, item);
     const int row0 = uniform_load(p.cu_q_len, b), end = uniform_load(p.cu_q_len, b + 1);
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
 template <int KIND, int D, bool FULL>
 hipError_t go(const PromptAttnParams &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.items * (unsigned)p.Hkv, (unsigned)p.max_chunks);
+    const dim3 grid((unsigned)p.items * (unsigned)p.Hkv + (p.errors != nullptr ? 1u : 0u), (unsigned)p.max_chunks);
     if constexpr (D == 128) {
         if (p.rows_log2 == 8) {
             hipLaunchKernelGGL((prompt_attn_kernel<KIND, D, FULL, 8>), grid, dim3(8 * kWave), 0, stream, p);

@@ -42,6 +42,8 @@ struct PromptAttnParams {
     float *acc, *ml;      // partial results [T * Hq][max_chunks][d], [..][2]
     unsigned long long *errors;
 };
+// Whether a request's rows, by offsets from device memory, are among the T packed ones, or there are none.
+__device__ __forceinline__ bool offsets_fit(int begin, int end, int T) { return begin == end || (begin >= 0 && end > begin && end <= T); }
 __host__ __device__ inline int row_item(int packed, int b, int group, int rows_log2) { return (int)(((int64_t)packed * group) >> rows_log2) + b; }
 hipError_t launch_prompt_attn(const PromptAttnParams &p, hipStream_t stream);
 
