@@ -468,8 +468,10 @@ spec_status spec_prefix_attn(const spec_prefix_attn_args *args, void *workspace,
  * Prompts and bounded caches.  The four calls below bring a prompt's rows to the cache and answer them, and keep a cache that grows
  * within bounds: spec_qk_norm_rope makes the rows that spec_kv_append or spec_kv8_append put into the pages, spec_prompt_attn is the
  * attention of any number of rows per request, spec_kv_weight says which tokens the rows looked at, and spec_kv_evict keeps those.
- * Limits: d in {64, 128}; pools, scales, weights and outputs 32-byte aligned, other rows 16-byte aligned.  Request slots with no rows
- * (q_len[b] == 0) are allowed everywhere, and so is a batch of them (T == 0: nothing is launched).
+ * Limits: d in {64, 128}; pools, scales, weights and outputs 32-byte aligned, other rows 16-byte aligned; Hq / Hkv <= 16, B <= 65535, Hkv <= 65535,
+ * T * Hq <= 2^30, T * (Hq / Hkv) < 2^28, contexts (and buckets) of up to 2^30 tokens, for spec_kv_evict tables of as many and pools of
+ * fewer than 2^27 pages, launches of fewer than 2^32 threads (SPEC_EUNSUPPORTED beyond them).
+ * Request slots with no rows (q_len[b] == 0) are allowed everywhere, and so is a batch of them (T == 0: nothing is launched).
  */
 
 /*

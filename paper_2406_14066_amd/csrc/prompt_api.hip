@@ -51,6 +51,16 @@ spec_status check_rope(const spec_qk_norm_rope_args *a)
     return SPEC_OK;
 }
 
+// The longest request that the launch allows for.
+int capacity_of(int B, int max_kv_len, const int32_t *host_kv_len, const int32_t *host_cu_q_len)
+{
+    if (max_kv_len > 0) return max_kv_len;
+    int most = 0;
+    for (int b = 0; b < B; ++b)
+        if (host_cu_q_len == nullptr || host_cu_q_len[b + 1] > host_cu_q_len[b]) most = std::max(most, host_kv_len[b]);
+    return most;
+}
+
 // What the attention and the weights have in common: query rows over paged K.
 spec_status check_rows(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t num_blocks, int32_t max_blocks_per_req, int32_t T, int32_t kv_dtype, int32_t kv_layout,
                        int32_t max_kv_len, int64_t q_token_stride, const void *q, const void *k_cache, const float *kv_scale, const int32_t *block_table,
@@ -75,19 +85,10 @@ spec_status check_rows(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t nu
         if (len < 0 || pages_of(len) > max_blocks_per_req || (max_kv_len > 0 && len > max_kv_len)) return SPEC_EINVAL;
     }
     if (d != 64 && d != 128) return SPEC_EUNSUPPORTED;
+    if (capacity_of(B, max_kv_len, host_kv_len, host_cu_q_len) > kMaxPacked) return SPEC_EUNSUPPORTED;   // (places of tokens, rounded up to steps and groups of them)
     if (Hq / Hkv > 16 || Hkv > kMostKvHeads || B > kMostGrid) return SPEC_EUNSUPPORTED;
     if ((int64_t)T * Hq > kMaxPacked || (int64_t)T * (Hq / Hkv) >= kMaxHeadRows) return SPEC_EUNSUPPORTED;   // (of T: whatever the offsets in device memory say)
     return SPEC_OK;
-}
-
-// The longest request that the launch allows for.
-int capacity_of(int B, int max_kv_len, const int32_t *host_kv_len, const int32_t *host_cu_q_len)
-{
-    if (max_kv_len > 0) return max_kv_len;
-    int most = 0;
-    for (int b = 0; b < B; ++b)
-        if (host_cu_q_len == nullptr || host_cu_q_len[b + 1] > host_cu_q_len[b]) most = std::max(most, host_kv_len[b]);
-    return most;
 }
 
 int kind_of(int32_t kv_dtype, int32_t kv_layout)
