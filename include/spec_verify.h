@@ -481,6 +481,7 @@ spec_status spec_prefix_attn(const spec_prefix_attn_args *args, void *workspace,
  * for the pairs i < rot_dim / 2 of a head's first rot_dim dims: (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved.
  * The other dims are y as it is.  Norms and products are fp32 (a row's sum of squares must be within its range), angles are 64-bit
  * products brought below a turn there; an output is rounded once.
+ * Limits: T <= 2^25, T * (Hq + Hkv) <= 2^30, (Hq + Hkv) * d < 2^31, rot_dim a multiple of 16 (SPEC_EUNSUPPORTED beyond them).
  * out_q may be q and out_k may be k (same address and stride, SPEC_EINVAL otherwise); apart from that outputs and inputs must not overlap.
  */
 typedef struct {

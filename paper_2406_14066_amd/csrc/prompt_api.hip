@@ -48,6 +48,7 @@ spec_status check_rope(const spec_qk_norm_rope_args *a)
     if (a->d != 64 && a->d != 128) return SPEC_EUNSUPPORTED;
     if (a->rot_dim % 16 != 0) return SPEC_EUNSUPPORTED;
     if ((int64_t)a->T * ((int64_t)a->Hq + a->Hkv) > kMaxPacked || a->T > 1 << 25) return SPEC_EUNSUPPORTED;
+    if (((int64_t)a->Hq + a->Hkv) * a->d >= (int64_t)1 << 31) return SPEC_EUNSUPPORTED;   // (a head's place in its token)
     return SPEC_OK;
 }
 
