@@ -510,7 +510,8 @@ spec_status spec_qk_norm_rope(const spec_qk_norm_rope_args *args, void *hip_stre
  * Softmax weights enter the product with V as fp32 values in as many 16-bit terms as that takes for SPEC_F32 outputs (bf16 pages three, 8-bit pages two), as one term for
  * SPEC_BF16 outputs (bf16 pages 8 bits, whose error is about a bf16 output's own rounding; 8-bit pages 11 bits).  Sums are not normalised until the end: |V| up to 2^90; scaled
  * scores up to 2^28.
- * An infinity or NaN in K or V reaches the rows that see it and no others.
+ * An infinity or NaN in K or V reaches the rows that see it and no others; an infinity of V stays one (or becomes NaN, for SPEC_BF16 outputs where its weight is below
+ * fp32's range).
  */
 typedef struct {
     int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;

@@ -244,7 +244,13 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     };
     // Infinities and NaN in V are cleared too; true: there were some.
     auto clear_odd = [&] {
-        uint32_t found = 0;
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 largest = {0, 0};   // magnitudes order as integers, infinities and NaN last
+#pragma unroll
+        for (int i = 0; i < PN; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, in.v[i][e] & 0x7FFF7FFFu));
+        if (__builtin_amdgcn_ballot_w64(max(largest.x, largest.y) >= 0x7F80) == 0) return false;
 #pragma unroll
         for (int i = 0; i < PN; ++i)
 #pragma unroll
@@ -252,9 +258,8 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
                 const uint32_t w = in.v[i][e];
                 const uint32_t lo = (w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, hi = (w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
                 in.v[i][e] = w & ~(lo | hi);
-                found |= lo | hi;
             }
-        return __builtin_amdgcn_ballot_w64(found != 0) != 0;
+        return true;
     };
     auto store = [&](int buf) {
         unsigned char *ks = sh.k[buf] + (my_page >> 1) * (KS * 1024) + (my_page & 1) * 256, *vs = sh.v[buf];
@@ -413,9 +418,9 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
             if (i + kAhead < 4 * SL) operand[i % kAhead] = read_v(buf, i + kAhead);
         }
     };
-    // bf16 pages, a step that some rows do not see whole: an infinity or NaN in V would reach those as 0 times it.  Such values are
-    // cleared on their way to LDS (see `clear_odd`), and the rows that see them get them here, from memory.
-    auto add_odd = [&](int t0) {
+    // bf16 pages, a step that some rows do not see whole: an infinity or NaN in V would reach those as 0 times it; and weights in several terms, some of them zero or
+    // negative, would make NaN of an infinity.  Such values are cleared on their way to LDS (see `clear_odd`), and the rows that see them get them here, from memory.
+    auto add_odd = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll 1
         for (int i = 0; i < min(kStepTokens, tok1 - t0); ++i) {
             const int entry = uniform_load(table, (t0 - tok0 + i) / SPEC_BLOCK_SIZE);
@@ -439,13 +444,14 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
         const int left = tok1 - tok0 - step * kStepTokens - my_page * SPEC_BLOCK_SIZE;
         if (left < SPEC_BLOCK_SIZE) clear_tail(left);
         if constexpr (!B8)
-            if (step >= seen_whole && clear_odd()) sh.odd[buf] = step;
+            if ((FULL || step >= seen_whole) && clear_odd()) sh.odd[buf] = step;
         store(buf);
     };
-    auto walk = [&](int u, auto masked) {
+    auto walk = [&](int u, auto masked) __attribute__((always_inline)) {
         const int buf = u & 1, t0 = tok0 + u * kStepTokens;
         __syncthreads();        // step u is in LDS, and no wavefront reads step u - 1 any more
         const bool active = masked ? t0 <= most : rows > 0;
+        const bool odd = !B8 && (masked || FULL) && sh.odd[buf] == u;
         if (active) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) operand[i] = read_k(buf, i);
@@ -461,8 +467,8 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
         product(buf, 0);
         weigh(buf, 1);
         product(buf, 1);
-        if constexpr (masked && !B8)
-            if (sh.odd[buf] == u) add_odd(t0);
+        if constexpr ((masked || FULL) && !B8)
+            if (odd) add_odd(t0);
     };
     if (tid < 2) sh.odd[tid] = -1;
     __syncthreads();
