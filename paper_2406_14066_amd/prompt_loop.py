@@ -7,8 +7,9 @@ The loop runs the library's entry points around prompts and bounded caches toget
                                   attention                      `spec_prompt_attn`, with each row's log-sum-exp
   a prompt's last rows say which of its tokens matter            `spec_kv_weight`
   a request with more tokens than the budget loses some          `spec_kv_evict`, into pages of its own; the old ones are free again
-  every step: the same with k + 1 rows a request (the weights are added to), then
+  every step: the same with k + 1 rows a request, then
               verification of the drafts                         `spec_reject_sample`
+              and what the rows that stay look at is added       `spec_kv_weight` (`accepted_only`; otherwise what all rows look at, before it)
 
 Positions go on counting when a cache has lost tokens.  There is no model around the steps: projections are Gaussian, the drafts
 and both models' logits are made as in the control loop.
@@ -30,14 +31,15 @@ from . import spec_verify as sv
 
 
 class PromptLoop:
-    """`requests` requests with prompts of prompt[0] .. prompt[1] tokens; `budget` tokens stay of each, the first `first` and the last `recent` among them."""
+    """`requests` requests with prompts of prompt[0] .. prompt[1] tokens; `budget` tokens stay of each, the first `first` and the last `recent` among them.
+    `accepted_only`: a step's weights are of the rows that verification leaves; otherwise of all its rows, rejected drafts' among them, before verification."""
 
     def __init__(self, requests, prompt, *, budget, chunk=1024, window=32, first=4, recent=64, k=4, steps=12, Hq=32, Hkv=8, d=128, V=4096, kv="bf16",
-                 layout=sv.KV_MFMA, sigma=0.773, seed=1, timed=False, device="cuda"):
+                 layout=sv.KV_MFMA, sigma=0.773, seed=1, timed=False, accepted_only=False, device="cuda"):
         import torch
         if min(requests, prompt[0], chunk, budget, window) < 1 or min(first, recent, k, steps) < 0 or prompt[1] < prompt[0]:
             raise ValueError("requests, prompts, chunk, budget and window must be positive, first, recent, k and steps not negative")
-        self.torch, self.device, self.seed, self.timed = torch, device, seed, timed
+        self.torch, self.device, self.seed, self.timed, self.accepted_only = torch, device, seed, timed, accepted_only
         self.B, self.chunk, self.window, self.first, self.recent, self.budget, self.k = requests, chunk, window, first, recent, budget, k
         self.Hq, self.Hkv, self.d, self.V, self.sigma, self.kv, self.layout = Hq, Hkv, d, V, sigma, kv, layout
         rng = np.random.default_rng(seed)
@@ -170,7 +172,8 @@ class PromptLoop:
         torch, B, k = self.torch, self.B, self.k
         T = B * (k + 1)
         out, lse = self._forward(np.full(B, k + 1, dtype=np.int32), self.step_seconds)
-        self._weigh(self.q, lse, self.host_len, self.cu, True)
+        if not self.accepted_only:
+            self._weigh(self.q, lse, self.host_len, self.cu, True)
         logits = torch.randn((T, self.V), generator=self.gen, device=self.device) * 3.0
         target = logits + torch.randn((T, self.V), generator=self.gen, device=self.device) * self.sigma
         drafts = logits[(torch.arange(T, device=self.device) + 1) % (k + 1) != 0]       # (a request's last row seeds its extra target row)
@@ -181,7 +184,11 @@ class PromptLoop:
                                              new_kv_len=self.new_kv_len)
         sv.spec_reject_sample(reject, sv.alloc_workspace(sv.spec_verify_workspace_bytes(None, reject), self.device))
         kept = self.new_kv_len.cpu().numpy().astype(np.int32)
-        self.position += kept - self.kept
+        stay = kept - self.kept
+        if self.accepted_only:      # (the tokens of rejected drafts are overwritten by the next step's, and their rows are in no sequence)
+            rows = torch.from_numpy(np.concatenate([np.arange(self.cu[b], self.cu[b] + stay[b]) for b in range(B)])).to(self.device)
+            self._weigh(self.q[rows], lse[rows], kept, np.concatenate([[0], np.cumsum(stay)]).astype(np.int32), True)
+        self.position += stay
         self.kept = kept
         self.step_index += 1
         return out, lse
@@ -206,7 +213,7 @@ def main():
     if not torch.cuda.is_available():
         print("prompt_loop: no GPU visible", file=sys.stderr)
         sys.exit(2)
-    loop = PromptLoop(args.requests, ((args.prompt + 1) // 2, args.prompt), budget=args.budget, chunk=args.chunk, k=args.k, steps=args.steps, kv=args.kv, timed=True)
+    loop = PromptLoop(args.requests, ((args.prompt + 1) // 2, args.prompt), budget=args.budget, chunk=args.chunk, k=args.k, steps=args.steps, kv=args.kv, timed=True, accepted_only=True)
     loop.take_prompts()
     loop.evict()
     for _ in range(args.steps):
