@@ -168,19 +168,22 @@ __global__ __launch_bounds__(waves_of(FORM) *kWave, FORM == kWeightSome ? 4 : 2)
                 for (int ks = 0; ks < KS; ++ks)
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                         *reinterpret_cast<const bf16x8 *>(row + (B8 ? 64 * (ks / 2) + 32 * half + 16 * (ks % 2) : 32 * ks + 16 * half)), k[ks], s, 0, 0, 0);
-                f32x4 parts = {0.0f, 0.0f, 0.0f, 0.0f};   // of the tile's 16 weights
+                f32x4 parts;   // of the tile's 16 weights
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4) {
                     const int at4 = i * kTileRows + 8 * e4 + 4 * half;
                     const f32x4 off = *reinterpret_cast<const f32x4 *>(&row_lse[buf][at4]);
                     if (all_see) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) parts[e] += fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
+                            parts[e] = e4 > 0 ? parts[e] + x : x;
+                        }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float x = fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e]));
-                            parts[e] += row_limit[buf][at4 + e] >= t0 + c32 ? x : 0.0f;
+                            const float all = fast_exp2(fmaf(s[4 * e4 + e], factor, -off[e])), x = row_limit[buf][at4 + e] >= t0 + c32 ? all : 0.0f;
+                            parts[e] = e4 > 0 ? parts[e] + x : x;
                         }
                     }
                 }

@@ -390,9 +390,8 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
             for (int r = 0; r < 4; ++r) {
                 const float x = s[h][4 * i + r];
                 const float e = fast_exp2(B8 ? x - m_use : fmaf(x, p.scale_log2, -m_use));
-                const float part = h + i > 0 ? l_step[r] : 0.0f;
-                if constexpr (B8) l_step[r] = fmaf(e, rv[r], part);
-                else l_step[r] = part + e;
+                if constexpr (B8) l_step[r] = h + i > 0 ? fmaf(e, rv[r], l_step[r]) : e * rv[r];
+                else l_step[r] = h + i > 0 ? l_step[r] + e : e;
                 float rest = e;
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) {
@@ -479,12 +478,16 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
     for (; u < min(steps, seen_whole); ++u) walk(u, std::false_type{});
     for (; u < steps; ++u) walk(u, std::true_type{});
 
-    // Results, and partial results where the tokens are split, go through LDS so that they go out in long pieces.
+    // Results, and partial results where the tokens are split, go through LDS so that they go out in long pieces.  (Which lane
+    // this is, is found again: no registers for that in the steps.)
+    int end_tid = threadIdx.x;
+    asm volatile("" : "+v"(end_tid));
+    const int end_lane = end_tid & 63, end_half = end_lane >> 5, end_c32 = end_lane & 31;
     l_run -= l_lost;
-    l_run += __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false)[half ^ 1]);
+    l_run += __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false)[end_half ^ 1]);
     const bool whole = chunks == 1;
     const size_t my_index = packed_row(p, row0, kvh, my_row);
-    if (half == 0 && c32 < rows) {
+    if (end_half == 0 && end_c32 < rows) {
         if (!whole) *reinterpret_cast<f32x2 *>(p.ml + (my_index * p.max_chunks + chunk) * 2) = (f32x2){m_run, l_run};
         else if (p.lse != nullptr) p.lse[my_index] = l_run == 0.0f ? -INFINITY : (m_run + __builtin_amdgcn_logf(B8 ? l_run * kLower : l_run)) * kLn2;
     }
@@ -509,11 +512,11 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const f32x16 &x = acc[d2 * (SL / 2) + sl];
-                    *reinterpret_cast<f32x4 *>(o + c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * half) * 4) = (f32x4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+                    *reinterpret_cast<f32x4 *>(o + end_c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * end_half) * 4) = (f32x4){x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
                 }
             lds_order();
 #pragma unroll
-            for (int piece = lane; piece < kWaveRows * OP; piece += kWave) {
+            for (int piece = end_lane; piece < kWaveRows * OP; piece += kWave) {
                 const int r = piece / OP, c = piece % OP;
                 if (r < rows) {
                     const size_t index = packed_row(p, row0, kvh, row_lo + r);
@@ -530,11 +533,11 @@ __global__ __launch_bounds__(W *kWave, D == 64 && !is_8bit(KIND) ? 3 : 2) void p
             for (int i = 0; i < 4; ++i) {
                 const f32x16 &x = acc[sl];
                 const f32x4 four = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                *reinterpret_cast<u32x2 *>(o + c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * half) * 2) = __builtin_bit_cast(u32x2, __builtin_convertvector(four, bf16x4));
+                *reinterpret_cast<u32x2 *>(o + end_c32 * Sh::kOutRow + (32 * sl + 8 * i + 4 * end_half) * 2) = __builtin_bit_cast(u32x2, __builtin_convertvector(four, bf16x4));
             }
         lds_order();
 #pragma unroll
-        for (int piece = lane; piece < kWaveRows * OP; piece += kWave) {
+        for (int piece = end_lane; piece < kWaveRows * OP; piece += kWave) {
             const int r = piece / OP, c = piece % OP;
             if (r < rows)
                 *reinterpret_cast<u32x4 *>(static_cast<__bf16 *>(p.out) + packed_row(p, row0, kvh, row_lo + r) * D + c * 8) =
