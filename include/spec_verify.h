@@ -508,8 +508,9 @@ spec_status spec_qk_norm_rope(const spec_qk_norm_rope_args *args, void *hip_stre
  * K and V are in the pages (spec_kv_append, spec_kv8_append).  A row whose position is negative sees no key: its output is zero and its
  * lse -infinity.  q is bf16, pages are bf16 in either layout or 8-bit codes with their scales.
  * Softmax weights enter the product with V as fp32 values in as many 16-bit terms as that takes for SPEC_F32 outputs (bf16 pages three, 8-bit pages two), as one term for
- * SPEC_BF16 outputs (bf16 pages 8 bits, whose error is about a bf16 output's own rounding; 8-bit pages 11 bits).  Sums are not normalised until the end: |V| up to 2^90; scaled
- * scores up to 2^28.
+ * SPEC_BF16 outputs (bf16 pages 8 bits, whose error is about a bf16 output's own rounding and comes on top of it, where spec_prefix_attn has 16; 8-bit pages 11 bits).  Sums of
+ * weights are fp32 with what their additions lose, whatever the length; sums of weights times V are plain fp32 sums of pages: with a V of one sign an fp32 output is off by up to a few
+ * 1e-5 after tens of thousands of tokens that are not split.  Sums are not normalised until the end: |V| up to 2^90; scaled scores up to 2^28.
  * An infinity or NaN in K or V reaches the rows that see it and no others; an infinity of V stays one (or becomes NaN, for SPEC_BF16 outputs where its weight is below
  * fp32's range).
  */
@@ -537,7 +538,8 @@ typedef struct {
     float softmax_scale;          /* 0 means 1/sqrt(d) */
 } spec_prompt_attn_args;
 size_t spec_prompt_attn_workspace_bytes(const spec_prompt_attn_args *args);   /* 0 if the arguments are malformed */
-/* A workspace smaller than that (256 bytes at least) serves too: tokens are then not split between blocks. */
+/* A workspace smaller than that (256 bytes at least) serves too: tokens are then not split between blocks, which takes few rows behind many tokens many times as long (one token behind
+ * 32000, 64/8 heads: 600 us in place of 37).  The size depends on the lengths and does not grow with the batch: ask for each batch of lengths, or give a bucket. */
 spec_status spec_prompt_attn(const spec_prompt_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
@@ -546,7 +548,8 @@ spec_status spec_prompt_attn(const spec_prompt_attn_args *args, void *workspace,
  * for all tokens t < kv_len[b], with the rows at the positions kv_len[b] - q_len[b] + j (give a prompt's last rows alone to ask what
  * those look at).  `before` is weight_in's value for tokens before kv_len[b] - q_len[b] and 0 for the rows' own tokens, or where weight_in is NULL.
  * Rows whose lse is not finite count nothing.  The weights of requests without rows stay as they are.  A page's weights are one request's: requests of
- * a call must not share pages (shared prompts: give them to a request of their own).  Sums are fp32, in an order that depends on the lengths alone.
+ * a call must not share pages (shared prompts: give them to a request of their own).  Sums are fp32, in an order that
+ * depends on the lengths and on the device's number of compute units.
  */
 typedef struct {
     int32_t B, Hq, Hkv, d, num_blocks, max_blocks_per_req, T;

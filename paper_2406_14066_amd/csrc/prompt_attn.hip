@@ -81,13 +81,16 @@ __device__ __forceinline__ size_t packed_row(const PromptAttnParams &p, int row0
 //   other without leaving its lane
 // The two pairs' score products take turns (chains on one accumulator wait for themselves: 16384 tokens 3982 -> 3890 us), operands are read six reads ahead.
 //
-// What bounds it: one prompt of 16384 tokens, 64/8 heads, d = 128, bf16: 3.85 ms, 1.14 PFLOP/s of visible pairs (a product of two 8192 x 8192 bf16
+// What bounds it: one prompt of 16384 tokens, 64/8 heads, d = 128, bf16: 3.8 .. 4.3 ms from card to card, 1.02 .. 1.15 PFLOP/s of visible pairs (a product of two 8192 x 8192 bf16
 // matrices 1.31).  Matrix cores are busy 55% of the cycles and vector instructions take 40% more; the two wavefronts of a SIMD are in the same phase
 // after each barrier.  The clock is 1.95 GHz under this load and falls further where the phases overlap more (half of the wavefronts half a step
 // behind: as many cycles, 4.0 .. 4.35 ms).  A block takes about 5 us to start and to end, which packed prompts of 700 .. 5000 tokens see ten times a
-// unit (420 us for 389 GFLOP).  Four wavefronts a block bring pages in twice as often (4.27 ms), but are done earlier where there are few.
-// Weights of bf16 outputs are one term: a second one of bf16 pages is half as many products again, for errors of 1.65e-3 instead of 2.1e-3 of the
-// output's norm; those of fp32 outputs three (8-bit pages: two), 2.6e-7.
+// unit (410 .. 460 us for 389 GFLOP).  Four wavefronts a block bring pages in twice as often (4.27 ms), but are done earlier where there are few.
+// Weights of bf16 outputs are one term: a second one of bf16 pages is half as many products again and their conversions, for errors of 1.65e-3 instead of 2.1e-3 of the
+// output's norm (16384 tokens 3.9 -> 5.4 ms, packed prompts 428 -> 573 us; for requests of up to 96 rows alone: one token behind 32000 37.7 -> 43 us, 64 of five rows, 64/8 heads, behind
+// 2000 128 -> 141, 8 of 1 .. 9 rows behind 2000 .. 30000 103 either way; a batch of both kinds up to a fifth more).  It goes by the types alone, so that a row's
+// error does not depend on what else is in the batch.  Those of fp32 outputs are three (8-bit pages: two): 2.6e-7 on Gaussian rows.  Each term's products are added to the sum by
+// themselves, the small ones rounded to its steps: with equal weights and a V of one sign up to 3.5e-5 of it after 16384 tokens that are not split.
 template <int KIND, int D, int W>
 struct PromptShared {
     static constexpr int kK = kStepTokens * D * 2;   // of a step
