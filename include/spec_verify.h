@@ -539,7 +539,7 @@ typedef struct {
 } spec_prompt_attn_args;
 size_t spec_prompt_attn_workspace_bytes(const spec_prompt_attn_args *args);   /* 0 if the arguments are malformed */
 /* A workspace smaller than that (256 bytes at least) serves too: tokens are then not split between blocks, which takes few rows behind many tokens many times as long (one token behind
- * 32000, 64/8 heads: 600 us in place of 37).  The size depends on the lengths and does not grow with the batch: ask for each batch of lengths, or give a bucket. */
+ * 32000, 64/8 heads: 600 us in place of 34).  The size depends on the lengths and does not grow with the batch: ask for each batch of lengths, or give a bucket. */
 spec_status spec_prompt_attn(const spec_prompt_attn_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*

@@ -637,13 +637,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptAttnParams p)
             for (int i = 0; i < N / 4; ++i) x[k][i] = *reinterpret_cast<const f32x4 *>(from + (size_t)min(c + k, chunks - 1) * D + i * 64);
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
-            const float w = c + k < chunks ? factors[wave][sub][c + k] : 0.0f;
-            if (w != 0.0f) {
+            const bool there = c + k < chunks;   // (a factor of zero counts: an infinity or NaN of tokens with weights below fp32's range is not lost)
+            const float w = factors[wave][sub][c + k];
 #pragma unroll
-                for (int i = 0; i < N / 4; ++i)
+            for (int i = 0; i < N / 4; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(w, x[k][i][e], sum[i][e]);
-            }
+                for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(w, there ? x[k][i][e] : 0.0f, sum[i][e]);
         }
     }
     const bool b8 = is_8bit(p.kind);

@@ -68,3 +68,33 @@ def test_small_weights_count_whatever_the_scale_of_v(rows, workspace, power, kin
         assert (np.abs(got[j, 0] - want) <= limit).all(), np.abs(got[j, 0] - want).max() / most
         # (a reference that includes V's scale, up to 119 + 16, known to 2^-23 of itself)
         assert abs(lse[j, 0] - np.log(weight[:see].sum())) <= 2.0 ** -21 * (abs(power) + 40)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["tiles", "tokens"])
+@pytest.mark.parametrize("workspace", [None, 256], ids=["split", "whole"])
+def test_odd_values_of_tokens_with_tiny_weights(workspace, kind, out):
+    """The first 1000 tokens have weights of e^-200, below fp32's range, in chunks of their own where the tokens are split: an infinity or NaN of
+    their V reaches the rows all the same (as itself or as NaN), and what else they hold counts nothing."""
+    print("case tiny weights", workspace, kind, out, flush=True)
+    rng = np.random.default_rng(73)
+    q_len, kv_len, Hq, Hkv, d = [3], [8000], 8, 1, 128
+    table, nb = R.tables(rng, kv_len)
+    cache = R.Cache(rng, nb, Hkv, d, kind)
+    q = np.zeros((3, Hq, d))
+    q[:, :, 0] = 1.0
+    for page in range(nb):
+        for slot in range(16):
+            cache.put(0, page, 0, slot, 0, 0.0)
+    for t in range(1000):
+        cache.put(0, table[0, t // 16], 0, t % 16, 0, -200.0)
+    cu = R.prefix_sum(q_len)
+    plain = P.reference(cache, q, table, kv_len, cu, 1.0)
+    for t, dim, value in ((10, 3, INF), (500, 77, -INF), (600, 90, NAN)):
+        cache.put(1, table[0, t // 16], 0, t % 16, dim, value)
+    got, lse, errors = P.run(cache, q, table, kv_len, cu, out, scale=1.0, workspace=workspace)
+    odd = np.zeros(d, dtype=bool)
+    odd[[3, 77, 90]] = True
+    assert errors == 0 and not np.isfinite(got[..., odd]).any()
+    assert not np.isposinf(got[..., 77]).any() and not np.isneginf(got[..., 3]).any() and np.isnan(got[..., 90]).all()
+    P.check(got[..., ~odd], lse, (plain[0][..., ~odd], plain[1], plain[2][..., ~odd], plain[3], plain[4]), out, kind, d)
