@@ -116,7 +116,7 @@ spec_status check_prompt(const spec_prompt_attn_args *a)
 // different times, which costs half of the longest one.  Each chunk of a row's tokens is a partial result to write and to read back; the
 // join is a launch and looks at the chunks in turn.  Measured, us, by chunks of the longest request (planned: *): one token behind 32000, 64/8
 // heads: 8 86, 16 52, 32 38 *, 64 45; 8 requests of 1 .. 9 rows behind 2000 .. 30000: 4 131, 8 104 *, 12 101, 24 109; 512 rows behind 8000: 1 206, 2 140 *, 3 167;
-// a prompt of 4000 tokens: 1 130 *, 2 156, 4 189.
+// a prompt of 4000 tokens: 1 130 *, 2 156, 4 189.  (With a join that took 4 us more for 32 chunks: the first is 34 now.)
 struct PromptPlan {
     int rows_log2, items, chunk_tokens, max_chunks, even, capacity;
     size_t acc, ml, total;   // offsets into the workspace
