@@ -363,6 +363,7 @@ spec_status spec_kv_weight(const spec_kv_weight_args *a, void *hip_stream)
     if (p.form == kWeightSome) {
         // As few groups as let all blocks run at once (two a unit), else two: four requests of 4500 .. 9400 tokens, by groups: 25.3, 22.1 *, 27.2, 33.8; of 8500: 30.8, 32.2, 28.7 *,
         // 34.1; two of 30000, int8: 44.2, 40.9, -, 39.8 *; 32/8 heads, sixteen of 4000 .. 12000: 73, 63.7 *, -, 64.6.
+        // Nine more batches that four groups do not fit (4 .. 64 requests of 1000 .. 30000 tokens, bf16, e4m3 and int8, 64/8, 32/8 and 32/32 heads), 1, 2, 3, 4 and 6 groups: two are within 6% of the best.
         auto blocks = [&](int groups) {
             int64_t n = 0;
             for (int b = 0; b < a->B; ++b)
